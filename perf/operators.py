@@ -125,16 +125,16 @@ def _held(x):
 
 
 def _cache_arrays(slots, heads, dim, block, gen):
-    """(codes, scales) of a cache of N(0, 1) rows: codes [slots, 2, heads, width], scales [blocks, 2, heads]."""
+    """(codes, scales) of a cache of N(0, 1) rows: codes [slots, 2, heads, width], scales [blocks, heads, 2]."""
     blocks, width = -(-slots // block), _width(dim)
     codes = torch.zeros(blocks * block, 2, heads, width, dtype=torch.uint8, device="cuda")
-    scales = torch.empty(blocks, 2, heads, device="cuda")
+    scales = torch.empty(blocks, heads, 2, device="cuda")
     step = max(1, (1 << 27) // (block * heads * dim))
     for lo in range(0, blocks, step):
         hi = min(blocks, lo + step)
         x = torch.randn((hi - lo), block, 2, heads, dim, generator=gen, device="cuda")
         e = _exponent(x.abs().amax((1, 4)))
-        scales[lo:hi] = torch.exp2(e)
+        scales[lo:hi] = torch.exp2(e).mT
         codes[lo * block:hi * block, ..., :dim] = _held(x * torch.exp2(-e)[:, None, :, :, None]).flatten(0, 1)
     return codes[:slots].contiguous(), scales
 
@@ -239,7 +239,7 @@ def _prepare_admit(case, gen):
     if case["repeats"]:
         ids[-case["repeats"]:] = ids[:case["repeats"]].clone()
     s = dict(remap=remap, node=node, weight=weight, ids=ids, codes=torch.zeros(slots, 2, 1, 16, dtype=torch.uint8, device="cuda"),
-             scales=torch.zeros(-(-slots // 16), 2, 1, device="cuda"), remap_now=remap.clone(),
+             scales=torch.zeros(-(-slots // 16), 1, 2, device="cuda"), remap_now=remap.clone(),
              count=torch.zeros(4, dtype=torch.int64, device="cuda"))
     for name in ("slot_of", "fresh", "fresh_slot"):
         s[name] = torch.zeros(ids.numel(), dtype=torch.int32, device="cuda")
@@ -304,7 +304,7 @@ def _cached_rows(s, slot, part):
     """fp32 rows [entries, heads, dim] of the cache; part 0: keys, 1: values."""
     c = s["case"]
     x = s["codes"][slot, part, :, :c["dim"]].view(torch.float8_e4m3fn).float()
-    return x * s["scales"][torch.div(slot, c["block"], rounding_mode="floor"), part][:, :, None]
+    return x * s["scales"][torch.div(slot, c["block"], rounding_mode="floor"), :, part][:, :, None]
 
 
 def _attend_plain(s):
@@ -350,15 +350,16 @@ def _attend_plain(s):
 def _store_plain(s):
     c = s["case"]
     slots, block, dim, at = c["slots"], c["block"], c["dim"], s["at"].long()
-    blocks = s["scales"].shape[0]
+    scales = s["scales"].mT
+    blocks = scales.shape[0]
     x = torch.stack([s["k"], s["v"]], 1).float()  # [n, 2, heads, dim]
     of = torch.div(at, block, rounding_mode="floor")
-    amax = torch.zeros_like(s["scales"])
+    amax = torch.zeros(scales.shape, device="cuda")
     amax.scatter_reduce_(0, of[:, None, None].expand(-1, 2, c["kv_heads"]), x.abs().amax(-1), "amax")
     count = torch.zeros(blocks, device="cuda").index_add_(0, of, torch.ones(at.numel(), device="cuda"))
     rows = torch.full((blocks,), float(block), device="cuda")
     rows[-1] = slots - (blocks - 1) * block
-    need, old = _exponent(amax), torch.log2(s["scales"])
+    need, old = _exponent(amax), torch.log2(scales)
     new = torch.where((count == rows)[:, None, None], need, torch.maximum(old, need))
     new = torch.where((count > 0)[:, None, None], new, old).round()
     back = s["back"].long()
@@ -457,7 +458,7 @@ def _attend_exact(s):
     def keys_and_values(slot):
         if not c["slots"]:
             return s["k"][slot].double(), s["v"][slot].double()
-        both = table[s["codes"][slot][..., :dim].long()] * s["scales"][slot // c["block"]].double()[..., None]
+        both = table[s["codes"][slot][..., :dim].long()] * s["scales"].mT[slot // c["block"]].double()[..., None]
         return both[..., 0, :, :], both[..., 1, :, :]
 
     longest = max([1] + [b - a for a, b in zip(bounds, bounds[1:])])
@@ -513,7 +514,7 @@ def _store_exact(s):
     amax = amax.view(-1, block, 2, c["kv_heads"]).amax(1)
     need = torch.ceil(torch.log2(amax.clamp(min=2.0 ** -140) / 448.0)).clamp(E_MIN, E_MAX)
     need = torch.where(448.0 * torch.exp2(need - 1) >= amax, (need - 1).clamp(min=E_MIN), need)
-    old = torch.log2(s["scales"].double())
+    old = torch.log2(s["scales"].mT.double())
     e = torch.where(kept.view(-1, block).any(1)[:, None, None], torch.maximum(old, need), need)
     e = torch.repeat_interleave(e, block, 0)
     old = torch.repeat_interleave(old, block, 0)
