@@ -269,7 +269,9 @@ enum {
   DCI_K_LINEAR = 8,      /* later layers: dense layer                               */
   DCI_K_COUNT_NODES = 9, /* pre-sampling: what DCI_K_WRITE_SRC is elsewhere, and the
                             visits of the input nodes (one kernel)                */
-  DCI_K_COUNT = 10
+  DCI_K_ATTN = 10,       /* attention over a block's lists                          */
+  DCI_K_KV = 11,         /* key/value cache: writing, reading, admission            */
+  DCI_K_COUNT = 12
 };
 #define DCI_TIMING_MAX_LAUNCHES 8192
 int32_t dci_timing_enable(dci_ctx* ctx, uint32_t class_mask);
@@ -455,6 +457,117 @@ int32_t dci_gather_forward(dci_ctx* ctx, const dci_graph* graph, const dci_cache
                            const dci_blocks* blocks, float* x, int32_t n_layers, const int32_t* dims,
                            int32_t model, const float* const* w_self, const float* const* w_neigh,
                            const float* const* bias, float* logits, uint64_t* stats);
+
+/* ---- attention over a block's lists, and the 8-bit key/value cache that serves it ------------- */
+
+/* Types of queries, outputs and dense rows. */
+#define DCI_F32 0
+#define DCI_BF16 1
+#define DCI_F16 2
+#define DCI_MAX_HEAD_DIM 256
+#define DCI_MAX_HEADS 128
+
+/* Keys and values of nodes, held in 8 bits: the counterpart of the feature cache for a model whose aggregator is attention.
+ * A slot holds the key and the value row of one node for every key head, as e4m3 codes (sign, four exponent bits, three mantissa
+ * bits, no infinities); `block` consecutive slots share a scale per head and kind, a power of two, and a code stands for its value
+ * times that scale.  The caller allocates the arrays (device memory) and empties them with dci_kv_clear(); slots are then filled
+ * with dci_kv_write(), at places of the caller's own choice or at those that dci_kv_admit() hands out. */
+typedef struct {
+  int64_t n_slots;    /* 1 .. 2^31-1                                                                       */
+  int32_t block;      /* slots that share a scale: a power of two, 1 .. 64; the last block may be shorter    */
+  int32_t kv_heads;   /* 1 .. DCI_MAX_HEADS                                                                */
+  int32_t head_dim;   /* 1 .. DCI_MAX_HEAD_DIM                                                             */
+  uint8_t* codes;     /* [n_slots, 2, kv_heads, W], W = head_dim rounded up to a multiple of 16, the columns behind
+                         head_dim zero; keys first, then values; 16-byte aligned                           */
+  float* scales;      /* [ceil(n_slots / block), kv_heads, 2]: of keys and of values; 0 = nothing written yet */
+  uint64_t* weight;   /* [n_slots] accumulated attention weight in units of 2^-32; 0 = the slot is free, and a slot
+                         that dci_kv_admit has given away has at least 1                                     */
+  int64_t* node;      /* [n_slots] the node whose rows the slot holds, or -1 (dci_kv_admit)                  */
+} dci_kv_cache;
+
+/* One attention call: the rows of a block attend over their lists of sources, as of dci_blocks (indptr = blk_indptr[h],
+ * src = blk_src[h], n_rows = cap_rows[h], n_dev = &counts[h], n_edges = cap_edges[h], max_list = the hop's fan-out) or any other lists of that
+ * form.  For a row i, a head h and the entries e = indptr[i] .. indptr[i+1] - 1 of its list, with K and V the rows that entry e names and
+ * head h / (n_heads / kv_heads) of them:
+ *   z_e = scale * (q_i . K_e) + bias_e;   p_e = exp(z_e - lse_i);   lse_i = log(sum exp z_e);   out_i = sum p_e V_e.
+ * An entry is left out where its bias is -inf or where what it names does not exist (a source outside [0, n_src), a slot outside
+ * [0, n_slots)): nothing of its rows is read, whatever they hold.  A row that has nothing left gives out = 0 and lse = -inf.
+ * Products, softmax statistics and sums are in fp32; out is rounded once to its type.  Sums run in an order that follows from the
+ * arguments alone, so a call that is made again gives the same bits. */
+typedef struct {
+  int64_t n_rows;          /* rows, or their bound where n_dev is given; 0 .. 2^31-1                     */
+  const int64_t* n_dev;    /* device: the number of rows (nullable); rows from there on are left as they are */
+  const int64_t* indptr;   /* device [n_rows + 1], ascending, within [0, n_edges]                      */
+  const int32_t* src;      /* device [n_edges]                                                         */
+  int64_t n_edges;         /* entries in src (a bound on indptr's last value)                          */
+  int64_t n_src;           /* sources: rows of dense k and v, entries of slots; 0 .. 2^31-1            */
+  int32_t max_list;        /* no list is longer, as by a fan-out; 0: not known.  Only the work split depends on it */
+  int32_t dtype;           /* DCI_F32, DCI_BF16 or DCI_F16: of q, out and dense k, v                   */
+  int32_t n_heads;         /* a multiple of kv_heads, at most DCI_MAX_HEADS                            */
+  int32_t kv_heads;
+  int32_t head_dim;        /* 1 .. DCI_MAX_HEAD_DIM                                                    */
+  float scale;             /* of the scores, usually 1 / sqrt(head_dim)                                */
+  const void* q;           /* device: row i, head h at i * q_stride + h * head_dim                     */
+  int64_t q_stride;        /* numbers from row to row, at least n_heads * head_dim                     */
+  void* out;               /* device, laid out like q; must not overlap any input                      */
+  int64_t out_stride;
+  float* lse;              /* device [n_rows, n_heads] (nullable)                                      */
+  const float* bias;       /* device [n_edges, bias_heads] (nullable)                                  */
+  int32_t bias_heads;      /* 1 (shared by the heads) or n_heads; 0 without bias                       */
+} dci_attn;
+
+/* Workspace of an attention call (accumulate as for dci_attn_cached): lists that are longer than a wavefront's share are split, and
+ * their parts joined from there; accumulated weights keep the scores there.  0 where max_list says that neither is needed.  It
+ * depends on n_rows, n_edges, max_list, heads and head_dim only. */
+size_t dci_attn_workspace_bytes(const dci_attn* attn, int32_t accumulate);
+
+/* Attention over dense rows (a model's later layers): source s, key head h at k + s * k_stride + h * head_dim, v likewise; strides in
+ * numbers, at least kv_heads * head_dim. */
+int32_t dci_attn_forward(dci_ctx* ctx, const dci_attn* attn, const void* k, int64_t k_stride, const void* v, int64_t v_stride);
+
+/* Attention over rows of the cache.  slots: device int32 [n_src], the slot of every source (as dci_kv_admit writes them for
+ * blocks->nodes), -1 for none; NULL: src holds slots, and n_src is not used.  accumulate != 0: cache->weight[s] += sum of p_e over the entries that name slot s, the
+ * rows and the heads.  An entry's sum over the heads is taken in fp32 (in parts, where there are many heads) and rounded to 2^-32; the additions
+ * are of integers, so their order does not matter.  A NaN adds nothing.  head_dim and kv_heads must be the cache's. */
+int32_t dci_attn_cached(dci_ctx* ctx, const dci_attn* attn, const dci_kv_cache* cache, const int32_t* slots, int32_t accumulate);
+
+/* Empties the cache: scales, weights and codes 0, nodes -1 (weight and node may be NULL). */
+int32_t dci_kv_clear(dci_ctx* ctx, const dci_kv_cache* cache);
+
+/* Writes rows of keys and values into the cache.  slots: device int32 [n_max], STRICTLY ASCENDING; entries outside [0, n_slots) are
+ * skipped, with their rows, and stand behind all others (fresh_slots of dci_kv_admit ends in such entries).  The number of rows is *n_dev (device
+ * int64) where n_dev is not NULL, n_max its bound.  k, v: device rows of `dtype`, row i, head h at i * stride + h * head_dim.
+ * For every block that the call writes to, head and kind: need = the least e with max |x| <= 448 * 2^e over the finite numbers written,
+ * within [-100, 119]; the block's scale becomes 2^need where the call writes every slot of the block or its scale is 0, and
+ * 2^max(need, old) otherwise.  Numbers are divided by the scale and rounded to the nearest e4m3 (ties to even; beyond 448 to
+ * 448); infinities and NaN become NaN.  Where the scale grows, the block's other slots are rounded anew: exactly, but for what
+ * falls below the smallest normal e4m3 (2^-6 of the scale).
+ * A call whose slots do not ascend so is an error that the next dci_sync reports (DCI_ERR_INVALID_ARG); what the blocks concerned
+ * then hold is not specified. */
+int32_t dci_kv_write(dci_ctx* ctx, const dci_kv_cache* cache, const int32_t* slots, int64_t n_max, const int64_t* n_dev, int32_t dtype,
+                     const void* k, int64_t k_stride, const void* v, int64_t v_stride);
+/* Reads rows back: row i of k and v (device, `dtype`) = what slot slots[i] holds, rounded to the type; rows of entries outside
+ * [0, n_slots) are left as they are.  Any order, repeats allowed. */
+int32_t dci_kv_read(dci_ctx* ctx, const dci_kv_cache* cache, const int32_t* slots, int64_t n_max, const int64_t* n_dev, int32_t dtype,
+                    void* k, int64_t k_stride, void* v, int64_t v_stride);
+
+/* Finds slots for the nodes of a batch, by eviction where there are no free ones (the dynamic counterpart of the fill: what the
+ * model attends to stays).  remap: device int32 [num_nodes], the slot of every node or -1; before the first call all -1, then kept up
+ * by these calls together with cache->node and cache->weight.  nodes: device int64 [n_max] (*n_dev of them where n_dev is not NULL), as
+ * blocks->nodes; a node may appear more than once, ids outside [0, num_nodes) are left alone (slot -1).
+ *   1. A node that has a slot keeps it (a hit): the slots of a call's own nodes are not taken away.
+ *   2. Every node without one, once, in the order of first appearance, is a miss.  The m = min(misses, slots that are not hit)
+ *      slots of least (weight, slot) among those not hit are given to the first m misses, in ascending order; free slots have weight 0 and so
+ *      go first.  The node that had such a slot loses it (remap = -1); weight becomes 1 and node the new node.
+ *   3. slots[i] (device int32 [n_max]) = the slot of nodes[i], -1 where there was none left.
+ *      fresh[j] (device int32 [n_max]) = the place in nodes of the j-th miss that got a slot, fresh_slots[j] its slot (ascending: what
+ *      dci_kv_write wants); both -1 from j = m on, up to n_max.
+ *      counts (device int64 [4]) = { m, misses, slots hit, nodes that lost their slot }.
+ * The rows of the new nodes are the caller's to write (dci_kv_write with fresh_slots) before they are attended to.  Workspace:
+ * dci_kv_admit_workspace_bytes(n_slots, n_max). */
+size_t dci_kv_admit_workspace_bytes(int64_t n_slots, int64_t n_max);
+int32_t dci_kv_admit(dci_ctx* ctx, const dci_kv_cache* cache, int32_t* remap, int64_t num_nodes, const int64_t* nodes, int64_t n_max,
+                     const int64_t* n_dev, int32_t* slots, int32_t* fresh, int32_t* fresh_slots, int64_t* counts);
 
 /* ---- inference over many batches, several in flight ----------------------------------------- */
 

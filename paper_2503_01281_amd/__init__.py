@@ -10,4 +10,5 @@ from .binding import (  # noqa: F401
     dci_fill_caches, dci_gather_features, dci_gnn_forward, dci_presample_count, dci_sage_forward, dci_sample_khop,
     dci_sample_khop_static, STATIC_SCRATCH_BYTES,
     library_path, load_library, pinned_empty, dci_probe_read, Lane, dci_infer_batches, dci_gather_forward, DCI_OPT_FUSED_INPUT, DCI_OPT_RELABEL_TILE_ITERS, DCI_OPT_INPUT_LAYER,
+    DCI_F32, DCI_BF16, DCI_F16, KvCache, dci_attn_forward, dci_attn_cached, dci_kv_write, dci_kv_read, dci_kv_admit,
 )

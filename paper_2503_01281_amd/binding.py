@@ -18,7 +18,7 @@ STAT = dict(edges_sampled=0, adj_node_hits=1, adj_node_misses=2, adj_edge_hits=3
             lines_bounds=12, lines_ids=13, rows_copied=14)
 
 KERNEL_CLASSES = ["table_clear", "sample", "relabel", "write_src", "gather", "mean_in", "linear_in", "mean", "linear",
-                  "count_nodes"]
+                  "count_nodes", "attn", "kv"]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libdci.so")
@@ -42,6 +42,18 @@ class _Cache(C.Structure):
                 ("cap_feat_bytes", C.c_uint64), ("adj_remap", C.c_void_p), ("c_indptr", C.c_void_p),
                 ("c_indices", C.c_void_p), ("adj_partial_node", C.c_int64), ("adj_partial_deg", C.c_int64),
                 ("feat_remap", C.c_void_p), ("feat_cache", C.c_void_p)]
+
+
+class _KvCache(C.Structure):
+    _fields_ = [("n_slots", C.c_int64), ("block", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("codes", C.c_void_p), ("scales", C.c_void_p), ("weight", C.c_void_p), ("node", C.c_void_p)]
+
+
+class _Attn(C.Structure):
+    _fields_ = [("n_rows", C.c_int64), ("n_dev", C.c_void_p), ("indptr", C.c_void_p), ("src", C.c_void_p), ("n_edges", C.c_int64),
+                ("n_src", C.c_int64), ("max_list", C.c_int32), ("dtype", C.c_int32), ("n_heads", C.c_int32), ("kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("scale", C.c_float), ("q", C.c_void_p), ("q_stride", C.c_int64), ("out", C.c_void_p),
+                ("out_stride", C.c_int64), ("lse", C.c_void_p), ("bias", C.c_void_p), ("bias_heads", C.c_int32)]
 
 
 class _Lane(C.Structure):
@@ -102,6 +114,16 @@ def load_library():
     lib.dci_gather_forward_workspace_bytes.restype = sz
     lib.dci_infer_batches.argtypes = [P, i32, P, P, P, i64, i32, i64, i64, P, i32, u64, i32, P, P, P, P, P, P]
     lib.dci_infer_batches.restype = i32
+    lib.dci_attn_workspace_bytes.argtypes = [P, i32]
+    lib.dci_attn_workspace_bytes.restype = sz
+    lib.dci_attn_forward.argtypes = [P, P, P, i64, P, i64]
+    lib.dci_attn_cached.argtypes = [P, P, P, P, i32]
+    lib.dci_kv_clear.argtypes = [P, P]
+    lib.dci_kv_write.argtypes = [P, P, P, i64, P, i32, P, i64, P, i64]
+    lib.dci_kv_read.argtypes = [P, P, P, i64, P, i32, P, i64, P, i64]
+    lib.dci_kv_admit_workspace_bytes.argtypes = [i64, i64]
+    lib.dci_kv_admit_workspace_bytes.restype = sz
+    lib.dci_kv_admit.argtypes = [P, P, P, i64, P, i64, P, P, P, P, P]
     lib.dci_probe_read.argtypes = [P, P, u64, i32, i32, i64, i32, u64, P, P]
     lib.dci_probe_read.restype = i32
     lib.dci_set_option.argtypes = [P, i32, i64]
@@ -109,7 +131,7 @@ def load_library():
     lib.dci_timing_read.argtypes = [P, P, P]
     for name in ("dci_set_option", "dci_timing_enable", "dci_timing_read", "dci_create", "dci_set_workspace", "dci_sync", "dci_blocks_bounds", "dci_presample_count",
                  "dci_fill_caches", "dci_sample_khop", "dci_gather_features", "dci_sage_forward",
-                 "dci_gnn_forward"):
+                 "dci_gnn_forward", "dci_attn_forward", "dci_attn_cached", "dci_kv_clear", "dci_kv_write", "dci_kv_read", "dci_kv_admit"):
         getattr(lib, name).restype = i32
     _lib = lib
     return lib
@@ -480,6 +502,128 @@ def dci_gather_forward(ctx: Context, graph: Graph, cache: Optional[Cache], block
     ctx.check(ctx.lib.dci_gather_forward(ctx.handle, C.byref(graph.c), None if cache is None else C.byref(cache.c),
                                          C.byref(blocks.c), _ptr(x), L, _i32_array(dims), int(model), arr(w_self),
                                          arr(w_neigh), arr(bias), _ptr(logits), _ptr(stats)))
+
+
+DCI_F32, DCI_BF16, DCI_F16 = 0, 1, 2
+_DTYPES = {torch.float32: DCI_F32, torch.bfloat16: DCI_BF16, torch.float16: DCI_F16}
+
+
+class KvCache:
+    """Keys and values of nodes in 8 bits (e4m3), ``block`` slots to a scale; see dci_kv_cache in dci.h.  Made empty.
+
+    ``codes`` uint8 [n_slots, 2, kv_heads, W] (W: head_dim on whole 16 bytes), ``scales`` fp32 [blocks, kv_heads, 2], ``weight`` int64
+    [n_slots] (accumulated attention weight in units of 2^-32), ``node`` int64 [n_slots]."""
+
+    def __init__(self, ctx: Context, n_slots: int, kv_heads: int, head_dim: int, block: int = 16):
+        dev = ctx.device
+        blocks, width = -(-int(n_slots) // int(block)), -(-int(head_dim) // 16) * 16
+        self._keep(torch.empty(n_slots, 2, kv_heads, width, dtype=torch.uint8, device=dev),
+                   torch.empty(blocks, kv_heads, 2, dtype=torch.float32, device=dev),
+                   torch.empty(n_slots, dtype=torch.int64, device=dev), torch.empty(n_slots, dtype=torch.int64, device=dev), head_dim, block)
+        self.clear(ctx)
+
+    def _keep(self, codes, scales, weight, node, head_dim, block):
+        self.codes, self.scales, self.weight, self.node = codes, scales, weight, node
+        self.n_slots, self.kv_heads, self.head_dim, self.block = codes.shape[0], codes.shape[2], int(head_dim), int(block)
+        self.c = _KvCache(self.n_slots, self.block, self.kv_heads, self.head_dim, _ptr(codes), _ptr(scales), _ptr(weight), _ptr(node))
+
+    @staticmethod
+    def from_arrays(codes: torch.Tensor, scales: torch.Tensor, weight: Optional[torch.Tensor], node: Optional[torch.Tensor],
+                    head_dim: int, block: int) -> "KvCache":
+        """Wraps cache arrays made elsewhere (device tensors, used in place)."""
+        assert codes.dtype == torch.uint8 and scales.dtype == torch.float32
+        assert codes.dim() == 4 and codes.shape[1] == 2 and codes.shape[3] == -(-head_dim // 16) * 16
+        assert scales.shape == (-(-codes.shape[0] // block), codes.shape[2], 2)
+        for t in (codes, scales, weight, node):
+            assert t is None or (t.is_cuda and t.is_contiguous())
+        for t in (weight, node):
+            assert t is None or (t.dtype == torch.int64 and t.numel() == codes.shape[0])
+        cache = KvCache.__new__(KvCache)
+        cache._keep(codes, scales, weight, node, head_dim, block)
+        return cache
+
+    def clear(self, ctx: Context):
+        ctx.check(ctx.lib.dci_kv_clear(ctx.handle, C.byref(self.c)))
+
+
+def _rows(t: torch.Tensor, heads: Optional[int] = None, head_dim: Optional[int] = None):
+    """(stride of the rows) of a tensor [n, heads, head_dim] whose rows are each in one piece."""
+    assert t.is_cuda and t.dtype in _DTYPES and t.dim() == 3
+    assert (heads is None or t.shape[1] == heads) and (head_dim is None or t.shape[2] == head_dim)
+    assert t.stride(2) == 1 or t.shape[2] == 1, "the columns of a head must be adjacent"
+    assert t.stride(1) == t.shape[2] or t.shape[1] == 1, "the heads of a row must be adjacent"
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1] * t.shape[2])
+
+
+def _attn_args(q, kv_heads, n_src, indptr, src, out, scale, lse, bias, n_dev, max_list):
+    n, heads, dim = q.shape
+    assert q.dtype == out.dtype and out.shape == q.shape
+    assert indptr.is_cuda and indptr.dtype == torch.int64 and indptr.is_contiguous() and indptr.numel() == n + 1
+    assert src.is_cuda and src.dtype == torch.int32 and src.is_contiguous()
+    assert lse is None or (lse.is_cuda and lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == (n, heads))
+    if bias is not None:
+        assert bias.is_cuda and bias.dtype == torch.float32 and bias.is_contiguous() and bias.dim() == 2 and bias.shape[0] == src.numel()
+    return _Attn(n, n_dev, _ptr(indptr), _ptr(src), src.numel(), n_src, int(max_list), _DTYPES[q.dtype], heads, kv_heads, dim, float(scale),
+                 _ptr(q), _rows(q), _ptr(out), _rows(out), _ptr(lse), _ptr(bias), 0 if bias is None else bias.shape[1])
+
+
+def dci_attn_forward(ctx: Context, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, indptr: torch.Tensor, src: torch.Tensor,
+                     out: torch.Tensor, scale: float, lse: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
+                     n_dev: Optional[int] = None, max_list: int = 0):
+    """Rows attend over their lists of dense rows: ``q``, ``out`` [n, n_heads, head_dim], ``k``, ``v`` [n_src, kv_heads, head_dim], of one
+    type (fp32, bf16 or fp16), rows strided as they like; ``indptr`` int64 [n + 1], ``src`` int32 [n_edges]; ``lse`` fp32 [n, n_heads];
+    ``bias`` fp32 [n_edges, 1 or n_heads].  ``n_dev``: device address of an int64 row count, n is then its bound; ``max_list``: no list
+    is longer (0: not known)."""
+    assert k.dtype == q.dtype and v.dtype == q.dtype and k.shape == v.shape
+    a = _attn_args(q, k.shape[1], k.shape[0], indptr, src, out, scale, lse, bias, n_dev, max_list)
+    need = ctx.lib.dci_attn_workspace_bytes(C.byref(a), 0)
+    if need:
+        ctx.ensure_workspace(need)
+    ctx.check(ctx.lib.dci_attn_forward(ctx.handle, C.byref(a), _ptr(k), _rows(k, head_dim=q.shape[2]), _ptr(v), _rows(v, head_dim=q.shape[2])))
+
+
+def dci_attn_cached(ctx: Context, q: torch.Tensor, cache: KvCache, indptr: torch.Tensor, src: torch.Tensor, out: torch.Tensor, scale: float,
+                    slots: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
+                    accumulate: bool = False, n_dev: Optional[int] = None, max_list: int = 0):
+    """dci_attn_forward over rows of the cache: entry e names slot ``slots[src[e]]`` (int32; -1: left out), or slot ``src[e]`` without
+    ``slots``.  ``accumulate`` adds the attention weights to ``cache.weight``."""
+    assert slots is None or (slots.is_cuda and slots.dtype == torch.int32 and slots.is_contiguous())
+    a = _attn_args(q, cache.kv_heads, 0 if slots is None else slots.numel(), indptr, src, out, scale, lse, bias, n_dev, max_list)
+    need = ctx.lib.dci_attn_workspace_bytes(C.byref(a), int(accumulate))
+    if need:
+        ctx.ensure_workspace(need)
+    ctx.check(ctx.lib.dci_attn_cached(ctx.handle, C.byref(a), C.byref(cache.c), _ptr(slots), int(accumulate)))
+
+
+def _kv_rows(cache, slots, k, v):
+    assert slots.is_cuda and slots.dtype == torch.int32 and slots.is_contiguous()
+    assert k.dtype == v.dtype and k.shape[0] >= slots.numel() and v.shape[0] >= slots.numel()
+    return _DTYPES[k.dtype], _ptr(k), _rows(k, cache.kv_heads, cache.head_dim), _ptr(v), _rows(v, cache.kv_heads, cache.head_dim)
+
+
+def dci_kv_write(ctx: Context, cache: KvCache, slots: torch.Tensor, k: torch.Tensor, v: torch.Tensor, n_dev: Optional[int] = None):
+    """Rows ``k``, ``v`` [n, kv_heads, head_dim] into the slots ``slots`` (int32 [n], strictly ascending, entries outside the cache last)."""
+    ctx.check(ctx.lib.dci_kv_write(ctx.handle, C.byref(cache.c), _ptr(slots), slots.numel(), n_dev, *_kv_rows(cache, slots, k, v)))
+
+
+def dci_kv_read(ctx: Context, cache: KvCache, slots: torch.Tensor, k: torch.Tensor, v: torch.Tensor, n_dev: Optional[int] = None):
+    """What the slots ``slots`` (int32 [n], any order) hold, into ``k``, ``v`` [n, kv_heads, head_dim]."""
+    ctx.check(ctx.lib.dci_kv_read(ctx.handle, C.byref(cache.c), _ptr(slots), slots.numel(), n_dev, *_kv_rows(cache, slots, k, v)))
+
+
+def dci_kv_admit(ctx: Context, cache: KvCache, remap: torch.Tensor, nodes: torch.Tensor, slots: torch.Tensor, fresh: torch.Tensor,
+                 fresh_slots: torch.Tensor, counts: torch.Tensor, n_dev: Optional[int] = None):
+    """Slots for the nodes of a batch, by eviction where there are no free ones: ``remap`` int32 [N] (kept up), ``nodes`` int64 [n];
+    written: ``slots``, ``fresh``, ``fresh_slots`` int32 [n], ``counts`` int64 [4] = (given, misses, hits, evicted)."""
+    n = nodes.numel()
+    for t in (remap, slots, fresh, fresh_slots):
+        assert t.is_cuda and t.dtype == torch.int32 and t.is_contiguous()
+    for t in (nodes, counts):
+        assert t.is_cuda and t.dtype == torch.int64 and t.is_contiguous()
+    assert slots.numel() >= n and fresh.numel() >= n and fresh_slots.numel() >= n and counts.numel() >= 4
+    ctx.ensure_workspace(ctx.lib.dci_kv_admit_workspace_bytes(cache.n_slots, n))
+    ctx.check(ctx.lib.dci_kv_admit(ctx.handle, C.byref(cache.c), _ptr(remap), remap.numel(), _ptr(nodes), n, n_dev, _ptr(slots), _ptr(fresh),
+                                   _ptr(fresh_slots), _ptr(counts)))
 
 
 class Lane:

@@ -10,8 +10,10 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libdci.so")
-SOURCES = ["dci_ctx.hip", "dci_sample.hip", "dci_gather.hip", "dci_sage.hip", "dci_layer.hip", "dci_fill.hip", "dci_probe.hip", "dci_pipeline.hip"]
-HEADERS = [os.path.join(CSRC, "dci_internal.h"), os.path.join(CSRC, "dci_parts.h"), os.path.join(CSRC, "dci_close.h"), os.path.join(ROOT, "include", "dci.h")]
+SOURCES = ["dci_ctx.hip", "dci_sample.hip", "dci_gather.hip", "dci_sage.hip", "dci_layer.hip", "dci_fill.hip", "dci_probe.hip", "dci_pipeline.hip",
+           "dci_attn.hip", "dci_kv.hip"]
+HEADERS = [os.path.join(CSRC, "dci_internal.h"), os.path.join(CSRC, "dci_parts.h"), os.path.join(CSRC, "dci_close.h"), os.path.join(CSRC, "dci_kv.h"),
+           os.path.join(ROOT, "include", "dci.h")]
 
 # Packed-fp32 instructions are switched off for all device code on purpose.
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",

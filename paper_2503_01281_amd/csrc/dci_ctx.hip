@@ -55,7 +55,9 @@ int32_t fill_bytes(dci_ctx* ctx, void* p, size_t bytes, uint32_t pattern) {
 
 int32_t check_device_flag(dci_ctx* ctx) {
   if (ctx->host_flag && *ctx->host_flag != 0u) {
+    const unsigned flag = *ctx->host_flag;
     *ctx->host_flag = 0u;
+    if (flag == 2u) return fail(ctx, DCI_ERR_INVALID_ARG, "dci_kv_write: slots must be strictly ascending, entries outside the cache behind all others");
     return fail(ctx, DCI_ERR_HIP,
                 "relabel scan timed out: a tile of the frontier scan waited longer than the spin limit for its "
                 "predecessors; the batch was voided (sizes zeroed) and its outputs must not be used");

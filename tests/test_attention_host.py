@@ -1,0 +1,93 @@
+"""What of the attention calls and the key/value cache needs no GPU: sizes, refusals without a context, and the reference that the GPU tests
+are held to against closed forms."""
+import ctypes as C
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from tests import attention_reference as ref
+
+
+@pytest.fixture(scope="module")
+def lib():
+    import paper_2503_01281_amd as dci
+    return dci.load_library()
+
+
+def test_calls_without_a_context_are_refused(lib):
+    from paper_2503_01281_amd import binding as b
+    a, c = b._Attn(), b._KvCache()
+    assert lib.dci_attn_forward(None, C.byref(a), None, 0, None, 0) == -1
+    assert lib.dci_attn_cached(None, C.byref(a), C.byref(c), None, 0) == -1
+    assert lib.dci_kv_clear(None, C.byref(c)) == -1
+    assert lib.dci_kv_write(None, C.byref(c), None, 0, None, 0, None, 0, None, 0) == -1
+    assert lib.dci_kv_read(None, C.byref(c), None, 0, None, 0, None, 0, None, 0) == -1
+    assert lib.dci_kv_admit(None, C.byref(c), None, 0, None, 0, None, None, None, None, None) == -1
+
+
+def test_workspace_sizes(lib):
+    from paper_2503_01281_amd import binding as b
+
+    def need(accumulate=0, **kw):
+        a = b._Attn(n_rows=100, n_edges=1500, n_src=10, max_list=15, n_heads=4, kv_heads=4, head_dim=64)
+        for k, v in kw.items():
+            setattr(a, k, v)
+        return lib.dci_attn_workspace_bytes(C.byref(a), accumulate)
+
+    up = lambda x: -(-x // 256) * 256
+    assert need() == 0                                     # short lists need none
+    assert need(1) == up(1500 * 4 * 4)                     # a score per entry and head
+    chunks = -(-1500 // 64)
+    parts = up(chunks * 2 * 4 * 2 * 4) + up(chunks * 2 * 4 * 64 * 4)
+    assert need(max_list=0) == need(max_list=65) == parts  # lists that may be longer than 64
+    assert need(1, max_list=0) == parts + up(1500 * 4 * 4) + up(100 * 4 * 4)
+    assert need(n_edges=0, max_list=0) == 0
+    for bad in (dict(n_rows=-1), dict(n_heads=3), dict(kv_heads=0), dict(head_dim=0), dict(head_dim=300), dict(n_edges=2 ** 40)):
+        assert need(1, **bad) == 0
+    assert lib.dci_attn_workspace_bytes(None, 0) == 0
+    assert 0 < lib.dci_kv_admit_workspace_bytes(1, 0) < lib.dci_kv_admit_workspace_bytes(10 ** 6, 10 ** 5)
+    assert lib.dci_kv_admit_workspace_bytes(0, 10) == 0 and lib.dci_kv_admit_workspace_bytes(10, -1) == 0
+
+
+def test_the_reference_rounds_as_torch_does():
+    x = torch.linspace(-460, 460, 40001).double()
+    want = x.clamp(-448, 448).to(torch.float8_e4m3fn).double().numpy()
+    assert np.array_equal(ref.to_e4m3(x.numpy()), want)
+    small = torch.linspace(-0.05, 0.05, 20001).double()
+    assert np.array_equal(ref.to_e4m3(small.numpy()), small.to(torch.float8_e4m3fn).double().numpy())
+    every = torch.arange(256, dtype=torch.int32).to(torch.uint8).view(torch.float8_e4m3fn).double().numpy()
+    assert np.array_equal(np.nan_to_num(ref.e4m3_values(), nan=1e9), np.nan_to_num(every, nan=1e9))
+    for amax in (448.0, 449.0, 224.0, 1e-3, 3.4e38, 1e-45):
+        e = ref.need_exponent(amax)
+        assert (448.0 * 2.0 ** e >= amax or e == 119) and (448.0 * 2.0 ** (e - 1) < amax or e == -100)
+
+
+def test_the_reference_attends_as_a_softmax_does():
+    rng = np.random.default_rng(1)
+    q, k, v = (rng.standard_normal((m, 4, 8)) for m in (3, 6, 6))
+    indptr, where = [0, 2, 2, 7], np.array([0, 5, 1, 1, -1, 2, 3])
+    bias = rng.standard_normal((7, 1))
+    bias[3] = -math.inf
+    out, lse, p, out_err, lse_err, p_err = ref.attend(q, k, v, indptr, where, 0.5, bias)
+    assert (out[1] == 0).all() and np.isneginf(lse[1]).all() and (p[3] == 0).all() and (p[4] == 0).all()
+    for i, e in ((0, [0, 1]), (2, [2, 5, 6])):
+        for h in range(4):
+            z = torch.from_numpy(k[where[e], h] @ q[i, h] * 0.5 + bias[e, 0])
+            w = torch.softmax(z, 0).numpy()
+            assert np.allclose(out[i, h], w @ v[where[e], h], rtol=0, atol=1e-14) and np.allclose(p[e, h], w, atol=1e-15)
+            assert abs(float(torch.logsumexp(z, 0)) - lse[i, h]) < 1e-14
+    assert 0 < out_err[0].max() < 1e-5 and 0 < lse_err[0].max() < 1e-5 and 0 < p_err.max() < 1e-5
+
+
+def test_the_reference_writes_and_admits():
+    held, exponents = np.zeros((4, 2, 1, 2)), np.full((2, 2, 1), -1000.0)
+    ref.write(held, exponents, [0], np.array([[[448.0, 1.0]]]), np.array([[[0.0, 0.0]]]), 4, 2)
+    assert exponents[0, 0, 0] == 0 and exponents[0, 1, 0] == -100 and held[0, 0, 0].tolist() == [448.0, 1.0]
+    ref.write(held, exponents, [1], np.array([[[900.0, 2.0]]]), np.array([[[1.0, 0.0]]]), 4, 2)  # the scale grows, slot 0 is rounded anew
+    assert exponents[0, 0, 0] == 2 and held[0, 0, 0].tolist() == [112.0, 0.25] and held[1, 0, 0].tolist() == [224.0, 0.5]
+    remap, node, weight = np.array([0, -1, 1, -1]), np.array([0, 2]), np.array([5, 3])
+    slots, fresh, fresh_slots, counts = ref.admit(remap, node, weight, np.array([3, 0, 3, 1]))
+    assert slots.tolist() == [1, 0, 1, -1] and fresh.tolist() == [0, -1, -1, -1] and fresh_slots.tolist() == [1, -1, -1, -1]
+    assert counts.tolist() == [1, 2, 1, 1] and remap.tolist() == [0, -1, -1, 1] and node.tolist() == [0, 3] and weight.tolist() == [5, 1]
