@@ -170,6 +170,14 @@ __device__ __forceinline__ float sum_lanes(float x, int log2) {
   if (log2 > 3) x += dpp<0x140>(x);  // the other half of sixteen, mirrored
   return x;
 }
+// The same for the maximum
+__device__ __forceinline__ float max_lanes(float x, int log2) {
+  if (log2 > 0) x = fmaxf(x, dpp<0xB1>(x));
+  if (log2 > 1) x = fmaxf(x, dpp<0x4E>(x));
+  if (log2 > 2) x = fmaxf(x, dpp<0x141>(x));
+  if (log2 > 3) x = fmaxf(x, dpp<0x140>(x));
+  return x;
+}
 
 }  // namespace dci
 

@@ -53,8 +53,6 @@ struct KvWrite {
   unsigned* host_flag;
 };
 
-constexpr int kWriteRows = 4;  // entries of the list that a wavefront looks for the beginnings of blocks in
-
 __device__ __forceinline__ bool is_number(float x) { return (__float_as_uint(x) & 0x7F800000u) != 0x7F800000u; }
 
 // The least e with amax <= 448 * 2^e, 448 = 1.75 * 2^8
@@ -85,94 +83,170 @@ __device__ __forceinline__ uint4 encode(const float (&x)[kChunk], int e) {
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// A wavefront to four entries of the list, a key head and a kind (keys or values).  It writes the blocks whose first entry is among its
-// four, whole: with 64 / LH rows at a time (LH lanes to a head of a row, 16 columns each) it takes the maximum of what is to be
-// written, settles the scale, rounds the block's other rows anew where that grew, and writes.  The list ascends, so a block's entries are
-// together, and no other wavefront touches this head and kind of the block.  What bounds it: the rows' bytes, read once where
-// a block's rows fit the wavefront (64 columns and 16 rows, say), twice, the second time from the L2, where they do not.
+// The block whose entries are rows [i, i + rows) of the list, for one head and kind, by a whole wavefront: first the maximum of what is to be
+// written, then the scale, the block's other rows where that grew, the rows.  mine: lane t's slot, -1 where it is none of the block's.
+template <int TYPE>
+__device__ void write_block(const KvWrite& a, int kind, int head, long long i, int mine) {
+  const int lane = lane_id(), lh = 1 << a.lh_log2, at_once = kWave >> a.lh_log2;
+  const int r = lane >> a.lh_log2, col = (lane & (lh - 1)) * kChunk, cols = min(kChunk, max(0, a.dim - col));
+  const int width = (a.dim + kChunk - 1) / kChunk * kChunk, block_slots = 1 << a.block_log2;
+  const char* from = a.from[kind] + ((long long)head * a.dim + col) * type_bytes(TYPE);
+  unsigned char* to = a.codes + (long long)(kind * a.kv_heads + head) * width + col;
+  const long long row_bytes = 2ll * a.kv_heads * width;
+  const unsigned long long with = __ballot(mine >= 0);
+  const int rows = with == ~0ull ? kWave : __builtin_ctzll(~with);
+  const int b = __shfl(mine, 0, kWave) >> a.block_log2;
+  const long long slot0 = (long long)b << a.block_log2;
+  const int block_rows = (int)min((long long)block_slots, a.n_slots - slot0);
+  float amax = 0.f, x[kChunk];
+  for (int t0 = 0; t0 < rows; t0 += at_once) {
+    const int t = t0 + r;
+    if (t < rows && cols > 0) {
+      read_chunk_as<TYPE>(from + (i + t) * a.stride[kind], cols, a.wide[kind], x);
+#pragma unroll
+      for (int j = 0; j < kChunk; ++j) amax = fmaxf(amax, is_number(x[j]) ? fabsf(x[j]) : 0.f);
+    }
+  }
+  for (int d = kWave / 2; d; d >>= 1) amax = fmaxf(amax, __shfl_xor(amax, d, kWave));
+  float* scale = a.scales + 2 * ((long long)b * a.kv_heads + head) + kind;
+  const float old = *scale;
+  int e = need_exp(amax);
+  if (rows < block_rows && old != 0.f) {
+    const int old_e = (int)(__float_as_uint(old) >> 23) - 127;
+    if (e > old_e) {
+      unsigned long long written = lane < rows ? 1ull << (mine & (block_slots - 1)) : 0ull;
+      for (int d = kWave / 2; d; d >>= 1) written |= __shfl_xor(written, d, kWave);
+      const float up = old * exp2_of(-e);  // 2^(old_e - e), or 0 far below
+      for (int t = r; t < block_rows; t += at_once) {
+        if (!((written >> t) & 1) && col < width) {
+          Chunk<kE4M3> c;
+          unsigned char* p = to + (slot0 + t) * row_bytes;
+          c.load(reinterpret_cast<const char*>(p), kChunk, true);
+          float y[kChunk];
+#pragma unroll
+          for (int j = 0; j < kChunk / 2; ++j) {
+            c.pair(j, y[2 * j], y[2 * j + 1]);
+            y[2 * j] *= up;
+            y[2 * j + 1] *= up;
+          }
+          *reinterpret_cast<uint4*>(p) = encode(y, 0);
+        }
+      }
+    } else {
+      e = old_e;
+    }
+  }
+  for (int t0 = 0; t0 < rows; t0 += at_once) {
+    const int t = t0 + r, s = __shfl(mine, min(t, kWave - 1), kWave);
+    if (t < rows && col < width) {
+#pragma unroll
+      for (int j = 0; j < kChunk; ++j) x[j] = 0.f;
+      if (cols > 0) read_chunk_as<TYPE>(from + (i + t) * a.stride[kind], cols, a.wide[kind], x);
+      *reinterpret_cast<uint4*>(to + (long long)s * row_bytes) = encode(x, e);
+    }
+  }
+  if (lane == 0) *scale = exp2_of(e);
+}
+
+// A wavefront to `rows` = T * 64 / LH entries of the list (LH lanes to a head of a row, 16 columns each), a key head and a kind (keys or
+// values).  It writes the blocks whose first entry is among its own, whole; the list ascends, so a block's entries are together, and no
+// other wavefront touches this head and kind of the block.  Where a row lies does not depend on its slot, so the rows are on their way while
+// the slots are looked at.  The blocks that end among the wavefront's entries are done side by side, their maxima joined in LDS; one that
+// goes on behind them, and one whose other rows have to be rounded anew, is done on its own (write_block).  What bounds it: the rows' bytes,
+// read and written once.
+template <int TYPE, int T>
 __global__ __launch_bounds__(kKvBlock) void k_kv_write(const KvWrite a) {
-  const int lane = lane_id();
-  const long long unit = (long long)blockIdx.x * kKvWaves + threadIdx.x / kWave;
+  const int lane = lane_id(), wave = (int)threadIdx.x / kWave;
+  const long long unit = (long long)blockIdx.x * kKvWaves + wave;
   const int parts = 2 * a.kv_heads;
   const int kind = (int)(unit % parts) & 1, head = (int)(unit % parts) >> 1;
-  const long long i0 = unit / parts * kWriteRows;
+  const int lh = 1 << a.lh_log2, at_once = kWave >> a.lh_log2, tile = T * at_once;
+  const long long i0 = unit / parts * tile;
   const long long n = a.n_dev ? min(a.n_max, max(0ll, *a.n_dev)) : a.n_max;
+  __shared__ unsigned peaks[kKvWaves][kWave];
   if (i0 >= n) return;
+  const int r = lane >> a.lh_log2, col = (lane & (lh - 1)) * kChunk, cols = min(kChunk, max(0, a.dim - col));
+  const int width = (a.dim + kChunk - 1) / kChunk * kChunk;
+  const char* from = a.from[kind] + ((long long)head * a.dim + col) * type_bytes(TYPE);
+  Chunk<TYPE> x[T];
+#pragma unroll
+  for (int k = 0; k < T; ++k) {
+    x[k].clear();
+    const long long i = i0 + k * at_once + r;
+    if (i < n && cols > 0) x[k].load(from + i * a.stride[kind], cols, a.wide[kind]);
+  }
   auto slot_at = [&](long long i) {
     const int s = i < n ? a.slots[i] : -1;
     return (unsigned)s < (unsigned long long)a.n_slots ? s : -1;
   };
-  bool first = false;
-  if (lane < kWriteRows) {
-    const int s = slot_at(i0 + lane);
-    const int before = i0 + lane > 0 ? slot_at(i0 + lane - 1) : -1;
-    first = s >= 0 && (before < 0 || (before >> a.block_log2) != (s >> a.block_log2));
-    if (s >= 0 && i0 + lane > 0 && (before < 0 || before >= s)) *a.host_flag = 2u;  // not ascending: dci_sync says so
-  }
-  unsigned long long firsts = __ballot(first);
-  const int lh = 1 << a.lh_log2, at_once = kWave >> a.lh_log2;
-  const int r = lane >> a.lh_log2, col = (lane & (lh - 1)) * kChunk, cols = min(kChunk, max(0, a.dim - col));
-  const int width = (a.dim + kChunk - 1) / kChunk * kChunk;
-  const char* from = a.from[kind] + ((long long)head * a.dim + col) * type_bytes(a.type);
-  unsigned char* to = a.codes + (long long)(kind * a.kv_heads + head) * width + col;
-  const long long row_bytes = 2ll * a.kv_heads * width;
-  while (firsts) {
-    const long long i = i0 + __builtin_ctzll(firsts);
-    firsts &= firsts - 1;
-    const int block_slots = 1 << a.block_log2;
-    const int mine = lane < block_slots ? slot_at(i + lane) : -1;
-    const int b = __shfl(mine, 0, kWave) >> a.block_log2;
-    const unsigned long long with = __ballot(mine >= 0 && (mine >> a.block_log2) == b);
-    const int rows = with == ~0ull ? kWave : __builtin_ctzll(~with);
-    const long long slot0 = (long long)b << a.block_log2;
-    const int block_rows = (int)min((long long)block_slots, a.n_slots - slot0);
-    float amax = 0.f, x[kChunk];
-    for (int t = r; t < rows + r; t += at_once) {  // (all lanes take the same turns)
+  const int s = lane < tile ? slot_at(i0 + lane) : -1;
+  const int before = i0 + lane > 0 && lane < tile ? slot_at(i0 + lane - 1) : -1;
+  const int behind = slot_at(i0 + tile);
+  peaks[wave][lane] = 0;
+  const bool is_first = s >= 0 && (before < 0 || (before >> a.block_log2) != (s >> a.block_log2));
+  if (s >= 0 && i0 + lane > 0 && (before < 0 || before >= s)) *a.host_flag = 2u;  // not ascending: dci_sync says so
+  const unsigned long long firsts = __ballot(is_first), real = __ballot(s >= 0);
+  if (!firsts) return;
+  const int count = real == ~0ull ? kWave : __builtin_ctzll(~real);  // entries before the first that is outside
+  const int last_first = kWave - 1 - __builtin_clzll(firsts);
+  // the last block, if it goes on behind these entries
+  const bool open = count == tile && behind >= 0 && behind >> a.block_log2 == __shfl(s, tile - 1, kWave) >> a.block_log2;
+  const unsigned long long closed = open ? firsts & ((1ull << last_first) - 1) : firsts;
+  auto first_of = [&](int row) {  // the first entry of a row's block, -1: not done here
+    const unsigned long long up_to = firsts & ((2ull << row) - 1);
+    if (!up_to || row >= count) return -1;
+    const int f = kWave - 1 - __builtin_clzll(up_to);
+    return (closed >> f) & 1 ? f : -1;
+  };
 #pragma unroll
-      for (int j = 0; j < kChunk; ++j) x[j] = 0.f;
-      if (t < rows && cols > 0) read_chunk(a.type, from + (i + t) * a.stride[kind], cols, a.wide[kind], x);
+  for (int k = 0; k < T; ++k) {
+    float amax = 0.f;
 #pragma unroll
-      for (int j = 0; j < kChunk; ++j) amax = fmaxf(amax, is_number(x[j]) ? fabsf(x[j]) : 0.f);
+    for (int j = 0; j < kChunk / 2; ++j) {
+      float y, z;
+      x[k].pair(j, y, z);
+      amax = fmaxf(amax, fmaxf(is_number(y) ? fabsf(y) : 0.f, is_number(z) ? fabsf(z) : 0.f));
     }
-    for (int d = kWave / 2; d; d >>= 1) amax = fmaxf(amax, __shfl_xor(amax, d, kWave));
+    amax = max_lanes(amax, a.lh_log2);
+    const int f = first_of(k * at_once + r);
+    if (f >= 0 && col == 0) atomicMax(&peaks[wave][f], __float_as_uint(amax));
+  }
+  __threadfence_block();
+  // lane f settles the scale of the block that begins with entry f
+  int e = 0;
+  bool apart = false;
+  if ((closed >> lane) & 1) {
+    const unsigned long long later = firsts >> 1 >> lane;
+    const int rows = (later ? lane + 1 + __builtin_ctzll(later) : count) - lane;
+    const int b = s >> a.block_log2;
+    const int block_rows = (int)min(1ll << a.block_log2, a.n_slots - ((long long)b << a.block_log2));
     float* scale = a.scales + 2 * ((long long)b * a.kv_heads + head) + kind;
     const float old = *scale;
-    int e = need_exp(amax);
+    e = need_exp(__uint_as_float(peaks[wave][lane]));
     if (rows < block_rows && old != 0.f) {
       const int old_e = (int)(__float_as_uint(old) >> 23) - 127;
-      if (e > old_e) {
-        unsigned long long written = lane < rows ? 1ull << (mine & (block_slots - 1)) : 0ull;
-        for (int d = kWave / 2; d; d >>= 1) written |= __shfl_xor(written, d, kWave);
-        const float up = old * exp2_of(-e);  // 2^(old_e - e), or 0 far below
-        for (int t = r; t < block_rows; t += at_once) {
-          if (!((written >> t) & 1) && col < width) {
-            Chunk<kE4M3> c;
-            unsigned char* p = to + (slot0 + t) * row_bytes;
-            c.load(reinterpret_cast<const char*>(p), kChunk, true);
-            float y[kChunk];
-#pragma unroll
-            for (int j = 0; j < kChunk / 2; ++j) {
-              c.pair(j, y[2 * j], y[2 * j + 1]);
-              y[2 * j] *= up;
-              y[2 * j + 1] *= up;
-            }
-            *reinterpret_cast<uint4*>(p) = encode(y, 0);
-          }
-        }
-      } else {
-        e = old_e;
-      }
+      apart = e > old_e;
+      e = max(e, old_e);
     }
-    for (int t = r; t < rows + r; t += at_once) {
-      if (rows > at_once) {
+    if (!apart) *scale = exp2_of(e);
+  }
+  const unsigned long long alone = __ballot(apart) | (open ? 1ull << last_first : 0ull);
 #pragma unroll
-        for (int j = 0; j < kChunk; ++j) x[j] = 0.f;
-        if (t < rows && cols > 0) read_chunk(a.type, from + (i + t) * a.stride[kind], cols, a.wide[kind], x);
-      }
-      const int s = __shfl(mine, min(t, kWave - 1), kWave);
-      if (t < rows && col < width) *reinterpret_cast<uint4*>(to + (long long)s * row_bytes) = encode(x, e);
+  for (int k = 0; k < T; ++k) {
+    const int row = k * at_once + r, f = first_of(row);
+    const int to_e = __shfl(e, max(f, 0), kWave), to_s = __shfl(s, row, kWave);
+    if (f >= 0 && !((alone >> f) & 1) && col < width) {
+      float y[kChunk];
+#pragma unroll
+      for (int j = 0; j < kChunk / 2; ++j) x[k].pair(j, y[2 * j], y[2 * j + 1]);
+      *reinterpret_cast<uint4*>(a.codes + ((2ll * to_s + kind) * a.kv_heads + head) * width + col) = encode(y, to_e);
     }
-    if (lane == 0) *scale = exp2_of(e);
+  }
+  for (unsigned long long todo = alone; todo; todo &= todo - 1) {
+    const long long i = i0 + __builtin_ctzll(todo);
+    int mine = lane < 1 << a.block_log2 ? slot_at(i + lane) : -1;
+    if (mine >= 0 && mine >> a.block_log2 != __shfl(mine, 0, kWave) >> a.block_log2) mine = -1;
+    write_block<TYPE>(a, kind, head, i, mine);
   }
 }
 
@@ -185,59 +259,90 @@ struct KvRead {
   int type;
   char* to[2];
   long long stride[2];
-  bool wide;
   const unsigned char* codes;
   const float* scales;
   long long n_slots;
   int block_log2, kv_heads, dim;
+  int lanes_log2;  // lanes to a row
 };
 
-// 16 bytes of the output to a lane where that goes (4 or 8 columns), else a number; lanes side by side along a row.  What bounds it: the
-// bytes written.
+// 16 bytes of the output to a lane where that goes (4 or 8 columns), else a number.  Lanes lie side by side along a row, `lanes` of them (a
+// power of two up to a workgroup) to a row, and a lane keeps its place in the rows; four rows at a time.  What bounds it: the bytes
+// written.
+template <int TYPE, bool WIDE>
 __global__ __launch_bounds__(kKvBlock) void k_kv_read(const KvRead a) {
+  constexpr int kPer = WIDE ? 16 / type_bytes(TYPE) : 1, kAtOnce = 4;
   const int width = (a.dim + kChunk - 1) / kChunk * kChunk;
-  const int per = a.wide ? 16 / type_bytes(a.type) : 1;
-  const unsigned head_pieces = (unsigned)(a.dim / per), row_pieces = 2u * a.kv_heads * head_pieces;
+  const unsigned head_pieces = (unsigned)a.dim / kPer, row_pieces = 2u * a.kv_heads * head_pieces;
   const long long n = a.n_dev ? min(a.n_max, max(0ll, *a.n_dev)) : a.n_max;
-  const long long all = n * row_pieces, step = (long long)gridDim.x * kKvBlock;
-  for (long long at = blockIdx.x * (long long)kKvBlock + threadIdx.x; at < all; at += step) {
-    const long long i = at / row_pieces;
-    const unsigned in = (unsigned)(at - i * row_pieces), part = in / head_pieces, col = (in - part * head_pieces) * per;
+  const int lanes = 1 << a.lanes_log2, rows = kKvBlock >> a.lanes_log2;
+  const long long step = (long long)gridDim.x * rows;
+  for (unsigned in = threadIdx.x & (lanes - 1); in < row_pieces; in += lanes) {
+    const unsigned part = in / head_pieces, col = (in - part * head_pieces) * kPer;
     const unsigned kind = part / (unsigned)a.kv_heads, head = part - kind * a.kv_heads;
-    const int s = a.slots[i];
-    if ((unsigned)s >= (unsigned long long)a.n_slots) continue;
-    const unsigned char* p = a.codes + ((2ll * s + kind) * a.kv_heads + head) * width + col;
-    const float scale = a.scales[2 * ((long long)(s >> a.block_log2) * a.kv_heads + head) + kind];
-    char* o = a.to[kind] + i * a.stride[kind] + ((long long)head * a.dim + col) * type_bytes(a.type);
-    if (a.wide) {
-      Chunk<kE4M3> c;
-      c.clear();
-      c.w[0].x = *reinterpret_cast<const unsigned*>(p);
-      if (per == 8) c.w[0].y = *reinterpret_cast<const unsigned*>(p + 4);
-      float y[8];
+    const unsigned char* codes = a.codes + (long long)part * width + col;
+    const float* scales = a.scales + 2 * head + kind;
+    char* to = (kind ? a.to[1] : a.to[0]) + ((long long)head * a.dim + col) * type_bytes(TYPE);
+    const long long stride = kind ? a.stride[1] : a.stride[0];
+    for (long long i0 = blockIdx.x * (long long)rows + (threadIdx.x >> a.lanes_log2); i0 < n; i0 += kAtOnce * step) {
+      int s[kAtOnce];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        c.pair(j, y[2 * j], y[2 * j + 1]);
-        y[2 * j] *= scale;
-        y[2 * j + 1] *= scale;
+      for (int k = 0; k < kAtOnce; ++k) {
+        s[k] = i0 + k * step < n ? a.slots[i0 + k * step] : -1;
+        if ((unsigned)s[k] >= (unsigned long long)a.n_slots) s[k] = -1;
       }
-      if (a.type == DCI_F32) *reinterpret_cast<float4*>(o) = make_float4(y[0], y[1], y[2], y[3]);
-      else if (a.type == DCI_BF16)
-        *reinterpret_cast<uint4*>(o) = make_uint4(two<DCI_BF16>(y[0], y[1]), two<DCI_BF16>(y[2], y[3]), two<DCI_BF16>(y[4], y[5]), two<DCI_BF16>(y[6], y[7]));
-      else
-        *reinterpret_cast<uint4*>(o) = make_uint4(two<DCI_F16>(y[0], y[1]), two<DCI_F16>(y[2], y[3]), two<DCI_F16>(y[4], y[5]), two<DCI_F16>(y[6], y[7]));
-    } else {
-      Chunk<kE4M3> c;
-      c.clear();
-      c.w[0].x = *p;
-      float y, unused;
-      c.pair(0, y, unused);
-      y *= scale;
-      if (a.type == DCI_F32) *reinterpret_cast<float*>(o) = y;
-      else if (a.type == DCI_BF16) *reinterpret_cast<unsigned short*>(o) = (unsigned short)two<DCI_BF16>(y, 0.f);
-      else *reinterpret_cast<unsigned short*>(o) = (unsigned short)two<DCI_F16>(y, 0.f);
+      Chunk<kE4M3> c[kAtOnce];
+      float scale[kAtOnce];
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) {
+        c[k].clear();
+        scale[k] = 0.f;
+        if (s[k] >= 0) {
+          const unsigned char* p = codes + s[k] * (2ll * a.kv_heads * width);
+          if (!WIDE) c[k].w[0].x = *p;
+          else if (kPer == 4) c[k].w[0].x = *reinterpret_cast<const unsigned*>(p);
+          else {
+            const uint2 u = *reinterpret_cast<const uint2*>(p);
+            c[k].w[0].x = u.x;
+            c[k].w[0].y = u.y;
+          }
+          scale[k] = scales[2ll * (s[k] >> a.block_log2) * a.kv_heads];
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) {
+        if (s[k] < 0) continue;
+        float y[8];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          c[k].pair(j, y[2 * j], y[2 * j + 1]);
+          y[2 * j] *= scale[k];
+          y[2 * j + 1] *= scale[k];
+        }
+        char* o = to + (i0 + k * step) * stride;
+        if (!WIDE) {
+          if (TYPE == DCI_F32) *reinterpret_cast<float*>(o) = y[0];
+          else *reinterpret_cast<unsigned short*>(o) = (unsigned short)two<TYPE>(y[0], 0.f);
+        } else if (TYPE == DCI_F32) {
+          *reinterpret_cast<float4*>(o) = make_float4(y[0], y[1], y[2], y[3]);
+        } else {
+          *reinterpret_cast<uint4*>(o) = make_uint4(two<TYPE>(y[0], y[1]), two<TYPE>(y[2], y[3]), two<TYPE>(y[4], y[5]), two<TYPE>(y[6], y[7]));
+        }
+      }
     }
   }
+}
+
+template <int TYPE>
+void launch_write(int tiles, const KvWrite& a, unsigned grid, hipStream_t stream) {
+  if (tiles == 1) hipLaunchKernelGGL((k_kv_write<TYPE, 1>), dim3(grid), dim3(kKvBlock), 0, stream, a);
+  else if (tiles == 2) hipLaunchKernelGGL((k_kv_write<TYPE, 2>), dim3(grid), dim3(kKvBlock), 0, stream, a);
+  else hipLaunchKernelGGL((k_kv_write<TYPE, 4>), dim3(grid), dim3(kKvBlock), 0, stream, a);
+}
+template <int TYPE>
+void launch_read(bool wide, const KvRead& a, unsigned grid, hipStream_t stream) {
+  if (wide) hipLaunchKernelGGL((k_kv_read<TYPE, true>), dim3(grid), dim3(kKvBlock), 0, stream, a);
+  else hipLaunchKernelGGL((k_kv_read<TYPE, false>), dim3(grid), dim3(kKvBlock), 0, stream, a);
 }
 
 int32_t check_rows(dci_ctx* ctx, const dci_kv_cache* cache, const int32_t* slots, int64_t n_max, int32_t dtype, const void* k, int64_t k_stride,
@@ -257,26 +362,34 @@ int32_t check_rows(dci_ctx* ctx, const dci_kv_cache* cache, const int32_t* slots
 
 // ---- admission ------------------------------------------------------------------------------------
 //
-// The m slots of least (weight, slot) among those that the batch does not use, by a radix selection over the weights: a first digit of 12 bits
-// that is a floating-point code of the weight (six bits of exponent, six of mantissa: weights differ in their order of magnitude, and a
-// digit of their highest bits would be the same for all), then as many digits of 12 bits of the rest as it takes until the slots
-// at the border are all alike or all wanted; a digit's counts are added up by workgroup in LDS, then in memory, and the workgroup
-// that ends last looks for the border.  Then slots and misses are numbered by prefix sums over tiles, and the j-th slot goes to the j-th
-// miss.  What bounds it: launches, and 8 bytes per slot and digit that mostly come from the last-level cache.
+// The m slots of least (weight, slot) among those that the batch does not use, by a radix selection over the weights: a first digit of 13 bits
+// that is a floating-point code of the weight (six bits of exponent, seven of mantissa: weights differ in their order of magnitude, and a
+// digit of their highest bits would be the same for all), then digits of 13 bits of the rest, until the slots at the border are all alike or
+// all wanted.  A digit's counts are added up by workgroup in LDS, then in memory; every workgroup of the next kernel looks for the border in them.  Three
+// digits tell weights apart that differ by 2^-33 of themselves (all of them below 16); what is left after that, one workgroup does by itself.
+// Slots and misses are kept as bit masks, numbered by prefix sums over tiles of them, and the j-th slot goes to the j-th miss.
+// Nothing waits for another workgroup: what a kernel leaves is looked through by every workgroup of the next (the counts of a digit, the sums of at
+// most 1,024 tiles).  What bounds it: nine launches one after the other, each a few dependent reads long, and 8 bytes per slot and digit that
+// mostly come from the last-level cache.
 
-constexpr int kDigit = 12, kBins = 1 << kDigit, kDigits = 6;  // 6 bits of exponent and mantissa each, then up to 57 others
-constexpr int kAdmitBlock = 256, kNodeTile = 1024, kSlotTile = 2048;
+constexpr int kDigit = 13, kBins = 1 << kDigit, kDigits = 3;
+constexpr int kMantissa = 7;  // of the first digit
+constexpr int kDigitBlock = 1024, kDigitSlots = 8;  // lanes; slots to a lane at a time
+constexpr int kAdmitBlock = 256, kStretch = 2048, kStretchWords = kStretch / 64;
+constexpr int kTiles = 1024;  // at most, of slots and of the batch
+constexpr int kHistBlocks = 256;
 
-struct AdmitState {
-  unsigned ticket[kDigits + 2];
-  unsigned hits, evicted;
-  unsigned misses;
-  unsigned want;  // m
-  // the border: slots with weight >> shift == prefix; `need` of the `have` such slots are taken, and all with a smaller weight
+// Slots with weight >> shift == prefix are at the border: `need` of them are taken, and all with a smaller weight
+struct Border {
   unsigned long long prefix;
   int shift;
-  unsigned need, have;
+  unsigned need;
   int done;
+};
+struct AdmitState {
+  Border border[kDigits];  // after digit 0, 1, and all
+  unsigned misses, hits;
+  unsigned want;  // m
 };
 
 struct Admit {
@@ -291,35 +404,34 @@ struct Admit {
   long long* counts;
   unsigned n_slots;
   AdmitState* st;
-  unsigned* hit;        // a bit per slot
-  unsigned* hist;       // [kDigits][kBins]
-  unsigned* node_tile;  // misses in a tile of nodes, then the sum of those before
-  unsigned long long* slot_tile;  // (smaller, at the border) likewise
-  int node_tiles, slot_tiles, hist_blocks;
+  unsigned* hit;                  // a bit per slot
+  unsigned* hist;                 // [kDigits][kBins]
+  unsigned* hit_part;             // [kHistBlocks] slots hit
+  unsigned long long* node_mask;  // a bit per place of the batch: a miss
+  unsigned* node_tile;            // misses in a tile of the batch
+  unsigned long long* slot_mask;  // [2] per 64 slots: weight below the border, at it
+  unsigned long long* slot_tile;  // (below, at) in a tile of slots, in the high and the low half
+  unsigned* gone_tile;            // nodes that lost their slot
+  int node_tiles, node_tile_blocks;    // tiles of the batch, kDigitBlock places times that many each
+  int slot_tiles, slot_tile_stretches; // tiles of slots, kStretch slots times that many each
+  int hist_blocks;
 };
 
 constexpr int kClaim = (int)0x80000000;  // remap of a node that place i of the batch asks a slot for: kClaim + i, below -1
 
 __device__ __forceinline__ unsigned first_digit(unsigned long long w) {
-  if (w < 64) return (unsigned)w;
+  if (w < 1u << kMantissa) return (unsigned)w;
   const int e = 63 - __builtin_clzll(w);
-  return (unsigned)((e - 5) * 64 + ((w >> (e - 6)) & 63));
-}
-
-template <class T>
-__device__ __forceinline__ T peek(const T* p) {
-  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-template <class T>
-__device__ __forceinline__ void put(T* p, T v) {
-  __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return (unsigned)(((e - kMantissa + 1) << kMantissa) + ((w >> (e - kMantissa)) & ((1 << kMantissa) - 1)));
 }
 
 __device__ __forceinline__ long long batch_size(const Admit& a) { return a.n_dev ? min(a.n_max, max(0ll, *a.n_dev)) : a.n_max; }
+__device__ __forceinline__ bool is_hit(const Admit& a, unsigned long long s) { return (a.hit[s >> 5] >> (s & 31)) & 1; }
 
 // Sum of x over the threads before this one, workgroup-wide; total: over all
+template <int BLOCK>
 __device__ unsigned long long block_before(unsigned long long x, unsigned long long* total) {
-  __shared__ unsigned long long sums[kAdmitBlock / kWave];
+  __shared__ unsigned long long sums[BLOCK / kWave];
   const unsigned long long incl = (unsigned long long)wave_incl_scan64((long long)x);
   const int wave = (int)threadIdx.x / kWave;
   __syncthreads();
@@ -327,7 +439,7 @@ __device__ unsigned long long block_before(unsigned long long x, unsigned long l
   __syncthreads();
   unsigned long long before = incl - x, all = 0;
 #pragma unroll
-  for (int w = 0; w < kAdmitBlock / kWave; ++w) {
+  for (int w = 0; w < BLOCK / kWave; ++w) {
     if (w < wave) before += sums[w];
     all += sums[w];
   }
@@ -335,236 +447,285 @@ __device__ unsigned long long block_before(unsigned long long x, unsigned long l
   return before;
 }
 
-// True in the workgroup that gets here last of `of`; what the others wrote before (with put, or atomics) is there for it
-__device__ bool last_here(unsigned* ticket, unsigned of) {
-  __shared__ bool last;
-  __threadfence();
-  __syncthreads();
-  if (threadIdx.x == 0) last = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == of - 1;
-  __syncthreads();
-  if (last) __threadfence();
-  return last;
-}
-
-// Tile sums become sums of the tiles before; returns the total (one workgroup)
-template <class T>
-__device__ T scan_tiles(T* tile, int n) {
-  unsigned long long carry = 0;
-  for (int t0 = 0; t0 < n; t0 += kAdmitBlock) {
-    const int t = t0 + (int)threadIdx.x;
-    const unsigned long long x = t < n ? (unsigned long long)peek(tile + t) : 0;
-    unsigned long long total;
-    const unsigned long long before = block_before(x, &total);
-    if (t < n) put(tile + t, (T)(carry + before));
-    carry += total;
-  }
-  return (T)carry;
+// Sums of the tiles before `tile`, workgroup-wide
+template <int BLOCK, class T>
+__device__ unsigned long long tiles_before(const T* tiles, int tile) {
+  unsigned long long sum = 0, total;
+  for (int t = (int)threadIdx.x; t < tile; t += BLOCK) sum += tiles[t];
+  (void)block_before<BLOCK>(sum, &total);
+  return total;
 }
 
 __global__ __launch_bounds__(kAdmitBlock) void k_admit_lookup(const Admit a) {
   const long long n = batch_size(a), i = blockIdx.x * (long long)kAdmitBlock + threadIdx.x;
-  bool new_hit = false;
-  if (i < n) {
-    const long long v = a.nodes[i];
-    if (v >= 0 && v < a.num_nodes) {
-      const int s = peek(a.remap + v);
-      if (s >= 0 && (unsigned)s < a.n_slots) {
-        const unsigned bit = 1u << (s & 31);
-        new_hit = !(atomicOr(a.hit + (s >> 5), bit) & bit);
-      } else {
-        atomicMin(a.remap + v, kClaim + (int)i);
-      }
-    }
-  }
-  const int hits = __popcll(__ballot(new_hit));
-  if (lane_id() == 0 && hits) atomicAdd(&a.st->hits, (unsigned)hits);
-}
-
-// Place i of the batch is the first of a node without a slot
-__device__ __forceinline__ bool is_miss(const Admit& a, long long i, long long n) {
-  if (i >= n) return false;
+  if (i >= n) return;
   const long long v = a.nodes[i];
-  return v >= 0 && v < a.num_nodes && a.remap[v] == kClaim + (int)i;
+  if (v < 0 || v >= a.num_nodes) return;
+  const int s = __hip_atomic_load(a.remap + v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  if (s >= 0 && (unsigned)s < a.n_slots) atomicOr(a.hit + (s >> 5), 1u << (s & 31));
+  else atomicMin(a.remap + v, kClaim + (int)i);
 }
 
-// One workgroup: the bin in which the need-th slot lies
-__device__ void find_border(const Admit& a, const unsigned* hist, int digit) {
-  AdmitState* st = a.st;
-  __shared__ unsigned found_bin, found_before;
-  if (threadIdx.x == 0) found_bin = 0xFFFFFFFFu;
-  __syncthreads();
-  const unsigned need = digit ? st->need : st->want;
-  unsigned long long carry = 0;
-  for (int b0 = 0; b0 < kBins; b0 += kAdmitBlock) {
-    const unsigned x = peek(hist + b0 + threadIdx.x);
-    unsigned long long total;
-    const unsigned long long before = carry + block_before(x, &total);
-    if (before < need && before + x >= need) {
-      found_bin = b0 + threadIdx.x;
-      found_before = (unsigned)before;
-    }
-    carry += total;
-  }
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    if (need == 0) {
-      st->prefix = 0;
-      st->shift = 0;
-      st->need = st->have = 0;
-      st->done = 1;
-    } else {
-      const unsigned bin = found_bin;
-      if (digit == 0) {
-        if (bin < 64) {
-          st->prefix = bin;
-          st->shift = 0;
+// Workgroup-wide: the bin of a digit's counts in which the need-th slot lies.  before: the border after the digit before, nullptr for the first.
+__device__ Border find_border(const unsigned* hist, unsigned need, const Border* before) {
+  constexpr int kPer = kBins / kDigitBlock;
+  __shared__ Border found;
+  unsigned x[kPer], sum = 0;
+#pragma unroll
+  for (int k = 0; k < kPer; ++k) sum += x[k] = hist[threadIdx.x * kPer + k];
+  unsigned long long total;
+  unsigned smaller = (unsigned)block_before<kDigitBlock>(sum, &total);
+  if (need == 0) {  // nothing is wanted: no weight is below 0, and none of those that are 0 is needed
+    if (threadIdx.x == 0) found = Border{0, 0, 0, 1};
+  } else if (smaller < need && smaller + sum >= need) {  // one lane
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+      if (smaller < need && smaller + x[k] >= need) {
+        const unsigned bin = threadIdx.x * kPer + k;
+        Border b;
+        if (!before) {
+          b.shift = bin >> kMantissa ? (int)(bin >> kMantissa) - 1 : 0;
+          b.prefix = bin >> kMantissa ? (1u << kMantissa) + (bin & ((1u << kMantissa) - 1)) : bin;
         } else {
-          st->prefix = 64 + (bin & 63);
-          st->shift = (int)(bin >> 6) - 1;
+          b.shift = max(0, before->shift - kDigit);
+          b.prefix = (before->prefix << (before->shift - b.shift)) + bin;
         }
-      } else {
-        const int shift = max(0, st->shift - kDigit);
-        st->prefix = (st->prefix << (st->shift - shift)) + bin;
-        st->shift = shift;
+        b.need = need - smaller;
+        b.done = b.shift == 0 || b.need == x[k];
+        found = b;
+        break;
       }
-      st->need = need - found_before;
-      st->have = peek(hist + bin);
-      st->done = st->shift == 0 || st->need == st->have;
+      smaller += x[k];
     }
   }
+  __syncthreads();
+  const Border b = found;
+  __syncthreads();
+  return b;
 }
 
-// Digit `digit` of the slots at the border; with the first one, workgroups of their own count the misses
-__global__ __launch_bounds__(kAdmitBlock) void k_admit_digit(const Admit a, int digit) {
-  AdmitState* st = a.st;
-  if (digit && st->done) return;
+// Counts of one digit over slots s0, s0 + step, ... into LDS, `kDigitSlots` at a time; returns the slots hit that it met
+template <bool FIRST>
+__device__ unsigned count_digit(const Admit& a, unsigned* bins, unsigned long long s0, unsigned long long step, unsigned long long prefix, int shift) {
+  const int low = max(0, shift - kDigit);
+  const unsigned mask = (1u << (shift - low)) - 1;
+  unsigned hits = 0;
+  for (unsigned long long s = s0; s < a.n_slots; s += step * kDigitSlots) {
+    unsigned long long w[kDigitSlots];
+    bool hit[kDigitSlots], real[kDigitSlots];
+#pragma unroll
+    for (int k = 0; k < kDigitSlots; ++k) {
+      const unsigned long long at = s + k * step;
+      real[k] = at < a.n_slots;
+      w[k] = real[k] ? a.weight[at] : 0;
+      hit[k] = real[k] && is_hit(a, at);
+    }
+#pragma unroll
+    for (int k = 0; k < kDigitSlots; ++k) {
+      if (hit[k]) ++hits;
+      else if (real[k]) {
+        if (FIRST) atomicAdd(&bins[first_digit(w[k])], 1u);
+        else if (w[k] >> shift == prefix) atomicAdd(&bins[(unsigned)(w[k] >> low) & mask], 1u);
+      }
+    }
+  }
+  return hits;
+}
+
+// The first digit of every slot's weight; workgroups beside mark the misses
+__global__ __launch_bounds__(kDigitBlock) void k_admit_first_digit(const Admit a) {
   __shared__ unsigned bins[kBins];
-  unsigned* hist = a.hist + digit * kBins;
+  unsigned long long total;
   if ((int)blockIdx.x < a.hist_blocks) {
-    for (int b = (int)threadIdx.x; b < kBins; b += kAdmitBlock) bins[b] = 0;
+    for (int b = (int)threadIdx.x; b < kBins; b += kDigitBlock) bins[b] = 0;
     __syncthreads();
-    const unsigned long long prefix = digit ? st->prefix : 0;
-    const int shift = digit ? st->shift : 0, low = max(0, shift - kDigit);
-    const unsigned step = (unsigned)a.hist_blocks * kAdmitBlock;
-    for (unsigned long long s = blockIdx.x * kAdmitBlock + threadIdx.x; s < a.n_slots; s += step) {
-      const unsigned long long w = a.weight[s];
-      const bool taken = (a.hit[s >> 5] >> (s & 31)) & 1;
-      if (!taken) {
-        if (!digit) atomicAdd(&bins[first_digit(w)], 1u);
-        else if (w >> shift == prefix) atomicAdd(&bins[(unsigned)(w >> low) & ((1u << (shift - low)) - 1)], 1u);
-      }
-    }
-    __syncthreads();
-    for (int b = (int)threadIdx.x; b < kBins; b += kAdmitBlock)
-      if (bins[b]) atomicAdd(hist + b, bins[b]);
-  } else {
-    const long long n = batch_size(a), i0 = (long long)(blockIdx.x - a.hist_blocks) * kNodeTile;
-    unsigned count = 0;
-    for (int k = 0; k < kNodeTile / kAdmitBlock; ++k) count += is_miss(a, i0 + k * kAdmitBlock + threadIdx.x, n) ? 1 : 0;
-    unsigned long long total;
-    (void)block_before(count, &total);
-    if (threadIdx.x == 0) put(a.node_tile + (blockIdx.x - a.hist_blocks), (unsigned)total);
-  }
-  if (!last_here(&st->ticket[digit], gridDim.x)) return;
-  if (!digit) {
-    const unsigned misses = scan_tiles(a.node_tile, a.node_tiles);
-    if (threadIdx.x == 0) {
-      st->misses = misses;
-      st->want = min(misses, a.n_slots - peek(&st->hits));
-    }
-    __syncthreads();
-  }
-  find_border(a, hist, digit);
-}
-
-// (weight below the border, at it) of a slot, in the high and the low half
-__device__ __forceinline__ unsigned long long side_of(const Admit& a, unsigned long long s, unsigned long long prefix, int shift) {
-  if (s >= a.n_slots || ((a.hit[s >> 5] >> (s & 31)) & 1)) return 0;
-  const unsigned long long p = a.weight[s] >> shift;
-  return p < prefix ? 1ull << 32 : p == prefix ? 1ull : 0ull;
-}
-
-// How many slots of every tile are taken, and the list of the misses that get one
-__global__ __launch_bounds__(kAdmitBlock) void k_admit_number(const Admit a) {
-  AdmitState* st = a.st;
-  if ((int)blockIdx.x < a.slot_tiles) {
-    const unsigned long long s0 = (unsigned long long)blockIdx.x * kSlotTile, prefix = st->prefix;
-    const int shift = st->shift;
-    unsigned long long sum = 0, total;
-    if (st->want)
-      for (int k = 0; k < kSlotTile / kAdmitBlock; ++k) sum += side_of(a, s0 + k * kAdmitBlock + threadIdx.x, prefix, shift);
-    (void)block_before(sum, &total);
-    if (threadIdx.x == 0) put(a.slot_tile + blockIdx.x, total);
-    if (last_here(&st->ticket[kDigits], (unsigned)a.slot_tiles)) (void)scan_tiles(a.slot_tile, a.slot_tiles);
+    const unsigned hits = count_digit<true>(a, bins, blockIdx.x * (unsigned long long)kDigitBlock + threadIdx.x, (unsigned long long)a.hist_blocks * kDigitBlock, 0, 0);
+    (void)block_before<kDigitBlock>(hits, &total);
+    if (threadIdx.x == 0) a.hit_part[blockIdx.x] = (unsigned)total;
+    for (int b = (int)threadIdx.x; b < kBins; b += kDigitBlock)
+      if (bins[b]) atomicAdd(a.hist + b, bins[b]);
     return;
   }
+  const int tile = (int)blockIdx.x - a.hist_blocks;
   const long long n = batch_size(a);
-  const unsigned want = st->want, tile = blockIdx.x - a.slot_tiles;
-  unsigned long long carry = a.node_tile[tile];
-  for (int k = 0; k < kNodeTile / kAdmitBlock; ++k) {
-    const long long i = (long long)tile * kNodeTile + k * kAdmitBlock + threadIdx.x;
-    const bool miss = is_miss(a, i, n);
-    unsigned long long total;
-    const unsigned long long j = carry + block_before(miss ? 1 : 0, &total);
-    if (miss && j < want) a.fresh[j] = (int)i;
-    if (i >= want && i < a.n_max) {
-      a.fresh[i] = -1;
-      a.fresh_slots[i] = -1;
+  unsigned misses = 0;
+  for (int k = 0; k < a.node_tile_blocks; ++k) {
+    const long long i = ((long long)tile * a.node_tile_blocks + k) * kDigitBlock + threadIdx.x;
+    bool miss = false;  // the first place of a node without a slot
+    if (i < n) {
+      const long long v = a.nodes[i];
+      miss = v >= 0 && v < a.num_nodes && a.remap[v] == kClaim + (int)i;
     }
-    carry += total;
+    const unsigned long long mask = __ballot(miss);
+    if (lane_id() == 0) a.node_mask[i >> 6] = mask;
+    misses += miss ? 1 : 0;
+  }
+  (void)block_before<kDigitBlock>(misses, &total);
+  if (threadIdx.x == 0) a.node_tile[tile] = (unsigned)total;
+}
+
+// The border after digit 0, as all workgroups of a kernel find it; the first one notes it, and the batch's figures
+__device__ Border first_border(const Admit& a) {
+  const unsigned misses = (unsigned)tiles_before<kDigitBlock>(a.node_tile, a.node_tiles);
+  const unsigned hits = (unsigned)tiles_before<kDigitBlock>(a.hit_part, a.hist_blocks);
+  const unsigned want = min(misses, a.n_slots - hits);
+  const Border b = find_border(a.hist, want, nullptr);
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    a.st->misses = misses;
+    a.st->hits = hits;
+    a.st->want = want;
+    a.st->border[0] = b;
+  }
+  return b;
+}
+
+// Digit 1 or 2 of the slots at the border
+__global__ __launch_bounds__(kDigitBlock) void k_admit_digit(const Admit a, int digit) {
+  __shared__ unsigned bins[kBins];
+  Border b;
+  if (digit == 1) {
+    b = first_border(a);
+  } else {
+    b = a.st->border[0];
+    if (!b.done) b = find_border(a.hist + kBins, b.need, &a.st->border[0]);
+    if (blockIdx.x == 0 && threadIdx.x == 0) a.st->border[1] = b;
+  }
+  if (b.done) return;
+  for (int k = (int)threadIdx.x; k < kBins; k += kDigitBlock) bins[k] = 0;
+  __syncthreads();
+  (void)count_digit<false>(a, bins, blockIdx.x * (unsigned long long)kDigitBlock + threadIdx.x, (unsigned long long)a.hist_blocks * kDigitBlock, b.prefix, b.shift);
+  __syncthreads();
+  for (int k = (int)threadIdx.x; k < kBins; k += kDigitBlock)
+    if (bins[k]) atomicAdd(a.hist + digit * kBins + k, bins[k]);
+}
+
+// One workgroup: the border after all digits
+__global__ __launch_bounds__(kDigitBlock) void k_admit_border(const Admit a) {
+  __shared__ unsigned bins[kBins];
+  __shared__ Border last;
+  Border b = a.st->border[1];
+  if (!b.done) b = find_border(a.hist + 2 * kBins, b.need, &a.st->border[1]);
+  while (!b.done) {
+    if (threadIdx.x == 0) last = b;
+    for (int k = (int)threadIdx.x; k < kBins; k += kDigitBlock) bins[k] = 0;
+    __syncthreads();
+    (void)count_digit<false>(a, bins, threadIdx.x, kDigitBlock, b.prefix, b.shift);
+    __syncthreads();
+    b = find_border(bins, b.need, &last);
+  }
+  if (threadIdx.x == 0) a.st->border[2] = b;
+}
+
+// Marks the slots below and at the border, and writes the list of the misses that get a slot
+__global__ __launch_bounds__(kAdmitBlock) void k_admit_number(const Admit a) {
+  const unsigned want = a.st->want;
+  if ((int)blockIdx.x < a.slot_tiles) {
+    const Border b = a.st->border[2];
+    unsigned long long sum = 0, total;
+    for (int stretch = 0; stretch < a.slot_tile_stretches; ++stretch) {
+      const unsigned long long s0 = ((unsigned long long)blockIdx.x * a.slot_tile_stretches + stretch) * kStretch + threadIdx.x;
+      unsigned long long p[kStretch / kAdmitBlock];
+      bool open[kStretch / kAdmitBlock];
+#pragma unroll
+      for (int k = 0; k < kStretch / kAdmitBlock; ++k) {
+        const unsigned long long s = s0 + k * kAdmitBlock;
+        open[k] = s < a.n_slots && want;
+        p[k] = open[k] ? a.weight[s] >> b.shift : 0;
+        open[k] = open[k] && !is_hit(a, s);
+      }
+#pragma unroll
+      for (int k = 0; k < kStretch / kAdmitBlock; ++k) {
+        const unsigned long long below = __ballot(open[k] && p[k] < b.prefix), at = __ballot(open[k] && p[k] == b.prefix);
+        if (lane_id() == 0) {
+          const unsigned long long word = (s0 + k * kAdmitBlock) >> 6;
+          a.slot_mask[2 * word] = below;
+          a.slot_mask[2 * word + 1] = at;
+          sum += ((unsigned long long)__popcll(below) << 32) + __popcll(at);
+        }
+      }
+    }
+    (void)block_before<kAdmitBlock>(sum, &total);
+    if (threadIdx.x == 0) a.slot_tile[blockIdx.x] = total;
+    return;
+  }
+  // places of the batch: as many as there are in a tile's workgroup
+  const long long at = (long long)(blockIdx.x - a.slot_tiles) * kDigitBlock;
+  const int tile = (int)(at / kDigitBlock / a.node_tile_blocks);
+  unsigned long long before = tiles_before<kAdmitBlock>(a.node_tile, tile), total;
+  {
+    unsigned sum = 0;
+    const long long w0 = (long long)tile * a.node_tile_blocks * (kDigitBlock / 64);
+    for (long long w = w0 + threadIdx.x; w < at / 64; w += kAdmitBlock) sum += (unsigned)__popcll(a.node_mask[w]);
+    (void)block_before<kAdmitBlock>(sum, &total);
+    before += total;
+  }
+  for (int k = 0; k < kDigitBlock / kAdmitBlock; ++k) {
+    const long long i = at + k * kAdmitBlock + threadIdx.x;
+    if (i < a.n_max && i >= want) a.fresh[i] = a.fresh_slots[i] = -1;
+    const unsigned long long mask = a.node_mask[i >> 6];
+    const bool miss = (mask >> (i & 63)) & 1;
+    unsigned long long j = before + __popcll(mask & ((1ull << (i & 63)) - 1));
+    for (long long w = at / 64; w < i >> 6; ++w) j += __popcll(a.node_mask[w]);
+    if (miss && j < want) a.fresh[j] = (int)i;
   }
 }
 
 // The j-th slot to the j-th miss
 __global__ __launch_bounds__(kAdmitBlock) void k_admit_give(const Admit a) {
-  AdmitState* st = a.st;
-  const unsigned want = st->want;
-  if (!want) return;
-  const unsigned long long prefix = st->prefix;
-  const int shift = st->shift;
-  const unsigned need = st->need;
-  constexpr int kPer = kSlotTile / kAdmitBlock;
-  const unsigned long long s0 = (unsigned long long)blockIdx.x * kSlotTile + threadIdx.x * kPer;
-  unsigned long long side[kPer], sum = 0;
-#pragma unroll
-  for (int k = 0; k < kPer; ++k) {
-    side[k] = side_of(a, s0 + k, prefix, shift);
-    sum += side[k];
-  }
-  unsigned long long total;
-  unsigned long long before = a.slot_tile[blockIdx.x] + block_before(sum, &total);
-  unsigned evicted = 0;
-#pragma unroll
-  for (int k = 0; k < kPer; ++k) {
-    const unsigned smaller = (unsigned)(before >> 32), equal = (unsigned)before;
-    if (side[k] >> 32 || (side[k] && equal < need)) {
-      const unsigned j = smaller + min(equal, need);
-      const int s = (int)(s0 + k);
-      const long long v = a.nodes[a.fresh[j]], old = a.node[s];
-      if (old >= 0 && old < a.num_nodes) {
-        a.remap[old] = -1;
-        ++evicted;
-      }
-      a.node[s] = v;
-      a.weight[s] = 1;
-      a.remap[v] = s;
-      a.fresh_slots[j] = s;
+  const unsigned want = a.st->want, need = a.st->border[2].need;
+  __shared__ unsigned long long words[kStretchWords][2], firsts[kStretchWords];  // masks; (below, at) before them
+  unsigned long long carry = tiles_before<kAdmitBlock>(a.slot_tile, (int)blockIdx.x), total;
+  unsigned lost = 0;
+  for (int stretch = 0; stretch < a.slot_tile_stretches && want; ++stretch) {
+    const unsigned long long s0 = ((unsigned long long)blockIdx.x * a.slot_tile_stretches + stretch) * kStretch;
+    unsigned long long x = 0;
+    const int w = (int)threadIdx.x;
+    if (w < kStretchWords) {
+      words[w][0] = a.slot_mask[2 * (s0 / 64 + w)];
+      words[w][1] = a.slot_mask[2 * (s0 / 64 + w) + 1];
+      x = ((unsigned long long)__popcll(words[w][0]) << 32) + __popcll(words[w][1]);
     }
-    before += side[k];
+    const unsigned long long before = block_before<kAdmitBlock>(x, &total);
+    if (w < kStretchWords) firsts[w] = carry + before;
+    carry += total;
+    __syncthreads();
+#pragma unroll 4
+    for (int k = 0; k < kStretch / kAdmitBlock; ++k) {
+      const int in = k * kAdmitBlock + (int)threadIdx.x, v_w = in >> 6;
+      const unsigned long long bit = 1ull << (in & 63);
+      const unsigned below = (unsigned)(firsts[v_w] >> 32) + (unsigned)__popcll(words[v_w][0] & (bit - 1));
+      const unsigned at = (unsigned)firsts[v_w] + (unsigned)__popcll(words[v_w][1] & (bit - 1));
+      if ((words[v_w][0] & bit) || ((words[v_w][1] & bit) && at < need)) {
+        const unsigned j = below + min(at, need);
+        const int s = (int)(s0 + in);
+        const long long v = a.nodes[a.fresh[j]], old = a.node[s];
+        if (old >= 0 && old < a.num_nodes) {
+          a.remap[old] = -1;
+          ++lost;
+        }
+        a.node[s] = v;
+        a.weight[s] = 1;
+        a.remap[v] = s;
+        a.fresh_slots[j] = s;
+      }
+    }
+    __syncthreads();
   }
-  (void)block_before(evicted, &total);
-  if (threadIdx.x == 0 && total) atomicAdd(&st->evicted, (unsigned)total);
+  (void)block_before<kAdmitBlock>(lost, &total);
+  if (threadIdx.x == 0) a.gone_tile[blockIdx.x] = (unsigned)total;
 }
 
 // The slots of the batch; claims that got none are taken back
 __global__ __launch_bounds__(kAdmitBlock) void k_admit_slots(const Admit a) {
   const long long n = batch_size(a), i = blockIdx.x * (long long)kAdmitBlock + threadIdx.x;
-  if (i == 0) {
-    const AdmitState* st = a.st;
-    a.counts[0] = st->want;
-    a.counts[1] = st->misses;
-    a.counts[2] = st->hits;
-    a.counts[3] = st->evicted;
+  if (blockIdx.x == 0) {
+    const unsigned long long total = tiles_before<kAdmitBlock>(a.gone_tile, a.slot_tiles);
+    if (threadIdx.x == 0) {
+      a.counts[0] = a.st->want;
+      a.counts[1] = a.st->misses;
+      a.counts[2] = a.st->hits;
+      a.counts[3] = (long long)total;
+    }
   }
   if (i >= n) return;
   const long long v = a.nodes[i];
@@ -579,18 +740,28 @@ __global__ __launch_bounds__(kAdmitBlock) void k_admit_slots(const Admit a) {
 
 struct AdmitSpace {
   AdmitState* st;
-  unsigned *hit, *hist, *node_tile;
-  unsigned long long* slot_tile;
-  size_t clear_bytes;  // from st on
+  unsigned *hist, *hit, *hit_part, *node_tile, *gone_tile;
+  unsigned long long *node_mask, *slot_mask, *slot_tile;
+  int node_tiles, node_tile_blocks, slot_tiles, slot_tile_stretches;
+  size_t clear_bytes;  // from hist on
 };
 AdmitSpace admit_space(Arena& ar, int64_t n_slots, int64_t n_max) {
   AdmitSpace s;
-  s.st = ar.take<AdmitState>(1);
+  const int64_t blocks = (n_max + kDigitBlock - 1) / kDigitBlock, stretches = (n_slots + kStretch - 1) / kStretch;
+  s.node_tile_blocks = (int)((blocks + kTiles - 1) / kTiles);
+  s.node_tiles = blocks ? (int)((blocks + s.node_tile_blocks - 1) / s.node_tile_blocks) : 0;
+  s.slot_tile_stretches = (int)((stretches + kTiles - 1) / kTiles);
+  s.slot_tiles = (int)((stretches + s.slot_tile_stretches - 1) / s.slot_tile_stretches);
   s.hist = ar.take<unsigned>((size_t)kDigits * kBins);
   s.hit = ar.take<unsigned>((size_t)(n_slots + 31) / 32);
   s.clear_bytes = ar.off;
-  s.node_tile = ar.take<unsigned>((size_t)(n_max + kNodeTile - 1) / kNodeTile);
-  s.slot_tile = ar.take<unsigned long long>((size_t)(n_slots + kSlotTile - 1) / kSlotTile);
+  s.st = ar.take<AdmitState>(1);
+  s.hit_part = ar.take<unsigned>(kHistBlocks);
+  s.node_mask = ar.take<unsigned long long>((size_t)s.node_tiles * s.node_tile_blocks * (kDigitBlock / 64));
+  s.node_tile = ar.take<unsigned>(kTiles);
+  s.slot_mask = ar.take<unsigned long long>((size_t)s.slot_tiles * s.slot_tile_stretches * kStretchWords * 2);
+  s.slot_tile = ar.take<unsigned long long>(kTiles);
+  s.gone_tile = ar.take<unsigned>(kTiles);
   return s;
 }
 
@@ -643,11 +814,17 @@ int32_t dci_kv_write(dci_ctx* ctx, const dci_kv_cache* cache, const int32_t* slo
   a.dim = cache->head_dim;
   a.lh_log2 = dci::log2_up((cache->head_dim + dci::kChunk - 1) / dci::kChunk);
   a.host_flag = ctx->host_flag;
-  const int64_t waves = (n_max + dci::kWriteRows - 1) / dci::kWriteRows * 2 * cache->kv_heads;
+  // entries to a wavefront: a block's, as far as four times the rows that it has lanes for go
+  const int at_once = dci::kWave >> a.lh_log2;
+  int tiles = 1;
+  while (tiles < 4 && tiles * at_once < cache->block) tiles *= 2;
+  const int64_t waves = (n_max + tiles * at_once - 1) / (tiles * at_once) * 2 * cache->kv_heads;
   const int64_t grid = (waves + dci::kKvWaves - 1) / dci::kKvWaves;
   if (grid > 0x7FFFFFFFll) return dci::fail(ctx, DCI_ERR_UNSUPPORTED, "key/value rows: too many rows and heads for one call");
   dci::Timed timed(ctx, DCI_K_KV);
-  hipLaunchKernelGGL(dci::k_kv_write, dim3((unsigned)grid), dim3(dci::kKvBlock), 0, ctx->stream, a);
+  if (dtype == DCI_F32) dci::launch_write<DCI_F32>(tiles, a, (unsigned)grid, ctx->stream);
+  else if (dtype == DCI_BF16) dci::launch_write<DCI_BF16>(tiles, a, (unsigned)grid, ctx->stream);
+  else dci::launch_write<DCI_F16>(tiles, a, (unsigned)grid, ctx->stream);
   DCI_LAUNCH_CHECK(ctx);
   return DCI_OK;
 }
@@ -669,18 +846,23 @@ int32_t dci_kv_read(dci_ctx* ctx, const dci_kv_cache* cache, const int32_t* slot
   a.to[1] = static_cast<char*>(v);
   a.stride[0] = k_stride * bytes;
   a.stride[1] = v_stride * bytes;
-  a.wide = dci::by_16_bytes(k, k_stride, cache->head_dim, dtype) && dci::by_16_bytes(v, v_stride, cache->head_dim, dtype);
+  const bool wide = dci::by_16_bytes(k, k_stride, cache->head_dim, dtype) && dci::by_16_bytes(v, v_stride, cache->head_dim, dtype);
   a.codes = cache->codes;
   a.scales = cache->scales;
   a.n_slots = cache->n_slots;
   a.block_log2 = dci::log2_up(cache->block);
   a.kv_heads = cache->kv_heads;
   a.dim = cache->head_dim;
-  const int64_t pieces = n_max * 2 * cache->kv_heads * (a.wide ? cache->head_dim * bytes / 16 : cache->head_dim);
-  int64_t grid = (pieces + dci::kKvBlock - 1) / dci::kKvBlock;
-  if (grid > (int64_t)ctx->num_cus * 64) grid = (int64_t)ctx->num_cus * 64;
+  const int64_t pieces = 2ll * cache->kv_heads * (wide ? cache->head_dim * bytes / 16 : cache->head_dim);
+  a.lanes_log2 = dci::log2_up(pieces);
+  if (a.lanes_log2 > 8) a.lanes_log2 = 8;  // a workgroup
+  const int64_t rows = dci::kKvBlock >> a.lanes_log2;
+  int64_t grid = (n_max + rows * 4 - 1) / (rows * 4);
+  if (grid > (int64_t)ctx->num_cus * 32) grid = (int64_t)ctx->num_cus * 32;
   dci::Timed timed(ctx, DCI_K_KV);
-  hipLaunchKernelGGL(dci::k_kv_read, dim3((unsigned)grid), dim3(dci::kKvBlock), 0, ctx->stream, a);
+  if (dtype == DCI_F32) dci::launch_read<DCI_F32>(wide, a, (unsigned)grid, ctx->stream);
+  else if (dtype == DCI_BF16) dci::launch_read<DCI_BF16>(wide, a, (unsigned)grid, ctx->stream);
+  else dci::launch_read<DCI_F16>(wide, a, (unsigned)grid, ctx->stream);
   DCI_LAUNCH_CHECK(ctx);
   return DCI_OK;
 }
@@ -724,25 +906,36 @@ int32_t dci_kv_admit(dci_ctx* ctx, const dci_kv_cache* cache, int32_t* remap, in
   a.st = sp.st;
   a.hit = sp.hit;
   a.hist = sp.hist;
+  a.hit_part = sp.hit_part;
+  a.node_mask = sp.node_mask;
   a.node_tile = sp.node_tile;
+  a.slot_mask = sp.slot_mask;
   a.slot_tile = sp.slot_tile;
-  a.node_tiles = (int)((n_max + dci::kNodeTile - 1) / dci::kNodeTile);
-  a.slot_tiles = (int)((cache->n_slots + dci::kSlotTile - 1) / dci::kSlotTile);
-  a.hist_blocks = a.slot_tiles < 128 ? a.slot_tiles : 128;
+  a.gone_tile = sp.gone_tile;
+  a.node_tiles = sp.node_tiles;
+  a.node_tile_blocks = sp.node_tile_blocks;
+  a.slot_tiles = sp.slot_tiles;
+  a.slot_tile_stretches = sp.slot_tile_stretches;
+  const int64_t per_block = dci::kDigitBlock * dci::kDigitSlots;
+  a.hist_blocks = (int)((cache->n_slots + per_block - 1) / per_block);
+  if (a.hist_blocks > dci::kHistBlocks) a.hist_blocks = dci::kHistBlocks;
   const unsigned node_blocks = (unsigned)(n_max > 0 ? (n_max + dci::kAdmitBlock - 1) / dci::kAdmitBlock : 1);
   dci::Timed timed(ctx, DCI_K_KV);
-  const int32_t filled = dci::fill_bytes(ctx, sp.st, sp.clear_bytes, 0);
+  const int32_t filled = dci::fill_bytes(ctx, sp.hist, sp.clear_bytes, 0);
   if (filled != DCI_OK) return filled;
-#define DCI_ADMIT(kernel_, grid_, ...)                                                                                       \
+#define DCI_ADMIT(kernel_, grid_, block_, ...)                                                                               \
   do {                                                                                                                       \
-    hipLaunchKernelGGL(kernel_, dim3((unsigned)(grid_)), dim3(dci::kAdmitBlock), 0, ctx->stream, ##__VA_ARGS__);             \
+    hipLaunchKernelGGL(kernel_, dim3((unsigned)(grid_)), dim3(block_), 0, ctx->stream, ##__VA_ARGS__);                       \
     DCI_LAUNCH_CHECK(ctx);                                                                                                   \
   } while (0)
-  DCI_ADMIT(dci::k_admit_lookup, node_blocks, a);
-  for (int digit = 0; digit < dci::kDigits; ++digit) DCI_ADMIT(dci::k_admit_digit, a.hist_blocks + (digit ? 0 : a.node_tiles), a, digit);
-  DCI_ADMIT(dci::k_admit_number, a.slot_tiles + a.node_tiles, a);
-  DCI_ADMIT(dci::k_admit_give, a.slot_tiles, a);
-  DCI_ADMIT(dci::k_admit_slots, node_blocks, a);
+  DCI_ADMIT(dci::k_admit_lookup, node_blocks, dci::kAdmitBlock, a);
+  DCI_ADMIT(dci::k_admit_first_digit, a.hist_blocks + a.node_tiles, dci::kDigitBlock, a);
+  DCI_ADMIT(dci::k_admit_digit, a.hist_blocks, dci::kDigitBlock, a, 1);
+  DCI_ADMIT(dci::k_admit_digit, a.hist_blocks, dci::kDigitBlock, a, 2);
+  DCI_ADMIT(dci::k_admit_border, 1, dci::kDigitBlock, a);
+  DCI_ADMIT(dci::k_admit_number, a.slot_tiles + (n_max + dci::kDigitBlock - 1) / dci::kDigitBlock, dci::kAdmitBlock, a);
+  DCI_ADMIT(dci::k_admit_give, a.slot_tiles, dci::kAdmitBlock, a);
+  DCI_ADMIT(dci::k_admit_slots, node_blocks, dci::kAdmitBlock, a);
 #undef DCI_ADMIT
   return DCI_OK;
 }
