@@ -516,13 +516,13 @@ typedef struct {
   int32_t bias_heads;      /* 1 (shared by the heads) or n_heads; 0 without bias                       */
 } dci_attn;
 
-/* Workspace of an attention call (accumulate as for dci_attn_cached): lists that are longer than a wavefront's share are split, and
- * their parts joined from there; accumulated weights keep the scores there.  0 where max_list says that neither is needed.  It
- * depends on n_rows, n_edges, max_list, heads and head_dim only. */
+/* Workspace of an attention call (accumulate as for dci_attn_cached): lists longer than 64 to 512 entries (the more entries there are in all, the
+ * longer) are cut, and their parts joined from there; with accumulate their scores are kept there.  0 where max_list says that there are no such
+ * lists.  It depends on n_rows, n_edges, max_list, heads, head_dim and accumulate only. */
 size_t dci_attn_workspace_bytes(const dci_attn* attn, int32_t accumulate);
 
 /* Attention over dense rows (a model's later layers): source s, key head h at k + s * k_stride + h * head_dim, v likewise; strides in
- * numbers, at least kv_heads * head_dim. */
+ * numbers, at least kv_heads * head_dim and below 2^30. */
 int32_t dci_attn_forward(dci_ctx* ctx, const dci_attn* attn, const void* k, int64_t k_stride, const void* v, int64_t v_stride);
 
 /* Attention over rows of the cache.  slots: device int32 [n_src], the slot of every source (as dci_kv_admit writes them for

@@ -3,11 +3,14 @@
 // For a row i and a head h, over the entries e of the row's list:  z_e = scale (q_i . K_e) + bias_e,  out = sum exp(z_e) V_e / sum exp(z_e).
 // One pass over the list: a running maximum m, the sum l of exp(z - m) and the accumulator of exp(z - m) V, the last two rescaled
 // when m grows.  Every K and V row that an entry names is read once, straight into registers, 16 columns to a lane:
-//   a head's columns lie in LH = 1 .. 16 adjacent lanes, the heads of a row side by side, P lanes in all (a power of two up to 64; more
+//   a head's columns lie in LH = 1 .. 16 adjacent lanes (the last lane takes the head's last 16 columns, whichever of them the lane before has as
+//   well: those count once in a score, and are written twice alike), the heads of a row side by side, P lanes in all (a power of two up to 64; more
 //   heads are shared out between wavefronts).  A score is a sum over LH lanes (DPP), and the lanes of a head then hold what they need
 //   for their columns of the output: nothing passes through LDS.
 //   The 64 / P groups of lanes of a wavefront work on rows of their own, or R of them on one row, each on every R-th entry, and join their
 //   (m, l, acc) at the row's end.
+//   A group's lanes look up P entries at a time, an entry to a lane, the next P while these are worked on; what an entry names then goes from its
+//   lane to all of them.  An entry that is left out takes row 0's place and a score of -inf.
 //   Query heads that share a key head are worked on together, up to four of them (GQ), from the same registers.
 // Lists longer than `chunk` entries are cut at multiples of it in the whole array of entries, so that neither the number nor the
 // length of lists needs to be known: a wavefront takes `chunk` entries, finds the rows they belong to (a 64-way search in indptr) and
@@ -23,6 +26,9 @@ namespace {
 
 constexpr int kAttnBlock = 256, kAttnWaves = kAttnBlock / kWave;
 constexpr float kLog2E = 1.44269504088896340736f;
+// wavefronts to a SIMD that the registers are shared out for
+template <int GQ>
+constexpr int kWavesPerSimd = GQ == 4 ? 2 : GQ == 2 ? 3 : 4;
 constexpr double kWeightUnit = 4294967296.0;  // 2^32
 
 struct Attn {
@@ -38,12 +44,11 @@ struct Attn {
   const char* q;
   char* out;
   long long q_stride, out_stride;  // bytes
-  bool q_wide, out_wide, kv_wide;
   float* lse;
   const float* bias;
   int bias_heads;
   const char *k, *v;
-  long long k_stride, v_stride;  // bytes
+  unsigned k_stride, v_stride;  // bytes
   const float* scales;           // the cache's, [block, kv head, 2]
   int block_log2, kv_heads;
   const int* slots;  // nullptr: src is the row of k and v
@@ -55,7 +60,7 @@ struct Attn {
   int gq_passes;                // of them, those that share a group
   int chunk;
   int n_chunks;  // 0: no list is cut
-  int chunk_blocks, row_blocks;
+  int stash_row;  // with weights: floats of LDS for the scores of an entry (an odd number, against bank conflicts), 0 without
   float* part_ml;   // [2 n_chunks, heads, 2]
   float* part_acc;  // [2 n_chunks, heads, W]
   float* all_lse;   // lse of the cut lists by row, accumulating only
@@ -64,12 +69,13 @@ struct Attn {
 // What a lane of an attention wavefront is there for
 struct Place {
   int sub;    // its group's number among those of a row
-  int col;    // its first column
-  int cols;   // its columns, 0: none
+  int part;   // its number among the head's lanes
+  int col;    // its first column: 16 * part, but that a head's last 16 columns, where they overlap those of the lane before, are its last lane's
+  bool some;  // whether there are columns for it
   int kv;     // its key head
   int head;   // its first query head
   int n_q;    // how many query heads
-  bool on;
+  int local;  // the first one's number within the wavefront
 };
 
 template <int GQ>
@@ -87,6 +93,7 @@ struct State {
 };
 
 __device__ __forceinline__ float exp_diff(float a, float b) { return __builtin_amdgcn_exp2f((a - b) * kLog2E); }
+__device__ __forceinline__ float log_of(float x) { return __builtin_amdgcn_logf(x) * 0.69314718055994530942f; }
 __device__ __forceinline__ float finite_or_0(float m) { return m == -INFINITY ? 0.f : m; }
 
 // The last row that begins at or before entry p (so the one that holds it, if one does); n >= 1, wavefront-wide
@@ -104,139 +111,149 @@ __device__ __forceinline__ long long row_of(const long long* __restrict__ indptr
   return lo;
 }
 
-__device__ __forceinline__ int slot_of(const Attn& a, int s) {
-  if ((unsigned)s >= a.n_src) return -1;
-  return a.slots ? a.slots[s] : s;
+// What entry-holding lane: the row of k and v that source s stands for, -1: none
+__device__ __forceinline__ int named(const Attn& a, int s) {
+  const bool in = (unsigned)s < a.n_src;
+  const int at = a.slots ? a.slots[in ? s : 0] : s;
+  return in && (unsigned)at < a.n_at ? at : -1;
 }
 
-// Entries [e0, e1) of one row, every (1 << r_log2)-th from e0 + sub on, into st
-template <int TYPE, int GQ, bool BIAS>
-__device__ __forceinline__ void attend(const Attn& a, const Place& pl, long long e0, long long e1, int r_log2, const float (&q)[GQ][kChunk],
-                                       State<GQ>& st) {
-  constexpr int U = TYPE == DCI_F32 ? 2 : 4;  // entries at a time
-  const int n = (int)min(e1 - e0, (long long)0x7FFFFFFF - 1024);
+// Entries [e0, e1) of one row into st: those of group `sub` are every (1 << r_log2)-th from e0 + sub on.  Returns what the lane's entry of the last
+// P << r_log2 named (there are no more where that is used).  stash (nullable): LDS for the scores, entry by entry of the wavefront; scores (nullable):
+// memory for them, entry by entry of the call.
+template <int TYPE, int GQ, bool BIAS, bool WIDE>
+__device__ __forceinline__ int attend(const Attn& a, const Place& pl, long long e0, long long e1, int r_log2, const float (&q)[GQ][kChunk],
+                                      State<GQ>& st, float* stash, float* scores) {
+  constexpr int U = TYPE == kE4M3 ? 4 : !WIDE ? 1 : TYPE == DCI_F32 ? 2 : 4;  // entries at a time
+  const bool any = a.n_at > 0 && a.n_src > 0;  // else no entry names anything
+  const int n = any ? (int)max(0ll, min(e1 - e0, 0x7FFFFFFFll - 8192)) : 0;
   const int* __restrict__ src = a.src + e0;
-  const int step = 1 << r_log2;
-  const long long k_off = (long long)pl.kv * a.dim * type_bytes(TYPE) + pl.col * type_bytes(TYPE);
-  const char* k0 = a.k + (TYPE == kE4M3 ? (long long)pl.kv * ((a.dim + kChunk - 1) / kChunk * kChunk) + pl.col : k_off);
-  const char* v0 = a.v + (TYPE == kE4M3 ? (long long)pl.kv * ((a.dim + kChunk - 1) / kChunk * kChunk) + pl.col : k_off);
-  int at[U], next[U];
+  const int lane = lane_id(), in = lane & ((1 << a.p_log2) - 1), base = lane - in;
+  const int batch = 1 << (a.p_log2 + r_log2), first = (in << r_log2) + pl.sub;
+  auto source = [&](int t) { return t < n ? src[t] : -1; };
+  int next = source(first), after = source(first + batch);
+  if (n > 0) next = named(a, next);
+  const int width = TYPE == kE4M3 ? (a.dim + kChunk - 1) / kChunk * kChunk : a.dim;
+  const unsigned offset = (unsigned)(pl.kv * width + pl.col) * type_bytes(TYPE);
+  const char *k0 = a.k + offset, *v0 = a.v + offset;
+  const char* s0 = reinterpret_cast<const char*>(a.scales + 2 * pl.kv);
+  const unsigned s_stride = 8u * a.kv_heads;
+  int now = -1;
+  for (int t0 = 0; t0 < n; t0 += batch) {
+    now = next;
+    next = named(a, after);
+    after = source(t0 + 2 * batch + first);
+    const int mine = min(1 << a.p_log2, (n - t0 - pl.sub + (1 << r_log2) - 1) >> r_log2);  // entries of this group
+    for (int u0 = 0; u0 < mine; u0 += U) {
+      Chunk<TYPE> kc[U], vc[U];
+      float ks[U], vs[U], bias[U][GQ];
+      bool there[U];
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const int t = pl.sub + u * step;
-    at[u] = t < n ? src[t] : -1;
-  }
-#pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const int t = pl.sub + (U + u) * step;
-    next[u] = t < n ? src[t] : -1;
-  }
-#pragma unroll
-  for (int u = 0; u < U; ++u) at[u] = slot_of(a, at[u]);
-  for (int t0 = 0; t0 < n; t0 += U * step) {
-    Chunk<TYPE> kc[U], vc[U];
-    float ks[U], vs[U], bias[U][GQ];
-    bool there[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int t = t0 + pl.sub + u * step;
-      there[u] = (unsigned)at[u] < a.n_at;
-      kc[u].clear();
-      vc[u].clear();
-      ks[u] = vs[u] = 1.f;
-      if (there[u] && pl.on) {
-        if (pl.cols > 0) {
-          kc[u].load(k0 + at[u] * a.k_stride, pl.cols, a.kv_wide);
-          vc[u].load(v0 + at[u] * a.v_stride, pl.cols, a.kv_wide);
+      for (int u = 0; u < U; ++u) {
+        const int at = __shfl(now, base + u0 + u, kWave);
+        there[u] = at >= 0;
+        const unsigned row = there[u] ? (unsigned)at : 0u;
+        ks[u] = vs[u] = 1.f;
+        if (WIDE || TYPE == kE4M3) {
+          kc[u].load(k0 + (unsigned long long)row * a.k_stride);
+          vc[u].load(v0 + (unsigned long long)row * a.v_stride);
+        } else {
+          kc[u].load(k0 + (unsigned long long)row * a.k_stride, a.dim, false);
+          vc[u].load(v0 + (unsigned long long)row * a.v_stride, a.dim, false);
         }
         if (TYPE == kE4M3) {
-          const float2 s = *reinterpret_cast<const float2*>(a.scales + 2 * ((long long)(at[u] >> a.block_log2) * a.kv_heads + pl.kv));
+          const float2 s = *reinterpret_cast<const float2*>(s0 + (unsigned long long)(row >> a.block_log2) * s_stride);
           ks[u] = s.x;
           vs[u] = s.y;
         }
-      }
-      if (BIAS) {
-#pragma unroll
-        for (int g = 0; g < GQ; ++g)
-          bias[u][g] = there[u] && pl.on && g < pl.n_q ? a.bias[(e0 + t) * a.bias_heads + (a.bias_heads > 1 ? pl.head + g : 0)] : 0.f;
-      }
-    }
-    // the slots of the entries after these, and the sources of those after them, on their way while these are worked on
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int t = t0 + pl.sub + (2 * U + u) * step;
-      at[u] = slot_of(a, next[u]);
-      next[u] = t < n ? src[t] : -1;
-    }
-    float z[U][GQ];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      float dot[GQ];
-#pragma unroll
-      for (int g = 0; g < GQ; ++g) dot[g] = 0.f;
-#pragma unroll
-      for (int j = 0; j < kChunk / 2; ++j) {
-        float x, y;
-        kc[u].pair(j, x, y);
-#pragma unroll
-        for (int g = 0; g < GQ; ++g) dot[g] = fmaf(q[g][2 * j + 1], y, fmaf(q[g][2 * j], x, dot[g]));
-      }
-#pragma unroll
-      for (int g = 0; g < GQ; ++g) {
-        z[u][g] = sum_lanes(dot[g], a.lh_log2) * (a.scale * ks[u]);
-        if (BIAS) z[u][g] = bias[u][g] == -INFINITY ? -INFINITY : z[u][g] + bias[u][g];
-        if (!there[u]) z[u][g] = -INFINITY;
-      }
-    }
-    if (a.scores && pl.col == 0 && pl.on) {
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int t = t0 + pl.sub + u * step;
-        if (t < n) {
+        if (BIAS) {
+          const int t = t0 + ((u0 + u) << r_log2) + pl.sub;
 #pragma unroll
           for (int g = 0; g < GQ; ++g)
-            if (g < pl.n_q) a.scores[(e0 + t) * a.heads + pl.head + g] = z[u][g];
+            bias[u][g] = there[u] && g < pl.n_q ? a.bias[(e0 + t) * a.bias_heads + (a.bias_heads > 1 ? pl.head + g : 0)] : 0.f;
         }
       }
-    }
-    float p[U][GQ];
-#pragma unroll
-    for (int g = 0; g < GQ; ++g) {
-      float m = st.m[g];
-#pragma unroll
-      for (int u = 0; u < U; ++u) m = fmaxf(m, z[u][g]);
-      const float base = finite_or_0(m), shrink = exp_diff(st.m[g], base);
-      st.m[g] = m;
-      st.l[g] *= shrink;
+      // (an entry after the other: numbers made of all entries' bytes ahead of their use would not fit the registers)
+      __builtin_amdgcn_sched_barrier(0);
+      float z[U][GQ];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        p[u][g] = exp_diff(z[u][g], base);
-        st.l[g] += p[u][g];
-        p[u][g] *= vs[u];
+#pragma unroll
+        for (int g = 0; g < GQ; ++g) z[u][g] = 0.f;
+#pragma unroll
+        for (int j = 0; j < kChunk / 2; ++j) {
+          float x, y;
+          kc[u].pair(j, x, y);
+#pragma unroll
+          for (int g = 0; g < GQ; ++g) z[u][g] = fmaf(q[g][2 * j + 1], y, fmaf(q[g][2 * j], x, z[u][g]));
+        }
+        __builtin_amdgcn_sched_barrier(0);
       }
+      sum_lanes<U * GQ>(&z[0][0], a.lh_log2);
 #pragma unroll
-      for (int j = 0; j < kChunk; ++j) st.acc[g][j] *= shrink;
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      // with a bias an entry may be left out for one head and not for the next: its values, whatever they are, then add nothing
-      bool in[GQ];
-#pragma unroll
-      for (int g = 0; g < GQ; ++g) in[g] = !BIAS || z[u][g] != -INFINITY;
-#pragma unroll
-      for (int j = 0; j < kChunk / 2; ++j) {
-        float x, y;
-        vc[u].pair(j, x, y);
+      for (int u = 0; u < U; ++u) {
 #pragma unroll
         for (int g = 0; g < GQ; ++g) {
-          if (in[g]) {
-            st.acc[g][2 * j] = fmaf(p[u][g], x, st.acc[g][2 * j]);
-            st.acc[g][2 * j + 1] = fmaf(p[u][g], y, st.acc[g][2 * j + 1]);
+          z[u][g] *= a.scale * ks[u];
+          if (BIAS) z[u][g] = bias[u][g] == -INFINITY ? -INFINITY : z[u][g] + bias[u][g];
+          if (!there[u]) z[u][g] = -INFINITY;
+        }
+        if (!there[u]) vc[u].clear();
+      }
+      if ((stash || scores) && pl.part == 0) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int t = t0 + ((u0 + u) << r_log2) + pl.sub;
+#pragma unroll
+          for (int g = 0; g < GQ; ++g) {
+            if (g < pl.n_q) {
+              if (stash) stash[(base + u0 + u) * a.stash_row + pl.local + g] = z[u][g];
+              if (scores && t < n) scores[(e0 + t) * a.heads + pl.head + g] = z[u][g];
+            }
           }
         }
       }
+      float p[U][GQ];
+#pragma unroll
+      for (int g = 0; g < GQ; ++g) {
+        float m = st.m[g];
+#pragma unroll
+        for (int u = 0; u < U; ++u) m = fmaxf(m, z[u][g]);
+        const float top = finite_or_0(m), shrink = exp_diff(st.m[g], top);
+        st.m[g] = m;
+        st.l[g] *= shrink;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          p[u][g] = exp_diff(z[u][g], top);
+          st.l[g] += p[u][g];
+          p[u][g] *= vs[u];
+        }
+#pragma unroll
+        for (int j = 0; j < kChunk; ++j) st.acc[g][j] *= shrink;
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        // with a bias an entry may be left out for one head and not for the next: its values, whatever they are, then add nothing
+        bool with[GQ];
+#pragma unroll
+        for (int g = 0; g < GQ; ++g) with[g] = !BIAS || z[u][g] != -INFINITY;
+#pragma unroll
+        for (int j = 0; j < kChunk / 2; ++j) {
+          float x, y;
+          vc[u].pair(j, x, y);
+#pragma unroll
+          for (int g = 0; g < GQ; ++g) {
+            if (with[g]) {
+              st.acc[g][2 * j] = fmaf(p[u][g], x, st.acc[g][2 * j]);
+              st.acc[g][2 * j + 1] = fmaf(p[u][g], y, st.acc[g][2 * j + 1]);
+            }
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
   }
+  return now;
 }
 
 // (m, l, acc) of lanes `apart` away joined into st
@@ -257,149 +274,191 @@ __device__ __forceinline__ void join_lanes(State<GQ>& st, int apart) {
   }
 }
 
-__device__ __forceinline__ void add_weight(const Attn& a, int s, float p) {
-  const int at = slot_of(a, s);
-  if (p > 0.f && (unsigned)at < a.n_at) atomicAdd(a.weight + at, (unsigned long long)((double)p * kWeightUnit + 0.5));
+__device__ __forceinline__ void add_weight(const Attn& a, int at, float p) {
+  if (p > 0.f && at >= 0) atomicAdd(a.weight + at, (unsigned long long)((double)p * kWeightUnit + 0.5));
 }
 
-template <int TYPE, int GQ, bool BIAS>
-__global__ __launch_bounds__(kAttnBlock, 2) void k_attn(const Attn a) {
-  const int lane = lane_id(), wave = (int)threadIdx.x / kWave;
-  const int p_lanes = 1 << a.p_log2, lh = 1 << a.lh_log2, groups = kWave >> a.p_log2;
-  const bool chunks = (int)blockIdx.x < a.chunk_blocks;
-  const long long unit0 = (long long)(chunks ? blockIdx.x : blockIdx.x - a.chunk_blocks) * kAttnWaves + wave;
-  const int pass = (int)(unit0 % a.passes);  // wavefronts side by side read the same rows
+// What a lane is there for in pass `pass` over the heads
+template <int GQ, bool WIDE>
+__device__ __forceinline__ Place place_of(const Attn& a, int pass, int r_log2, int* heads_here, int* n_q) {
+  const int in = lane_id() & ((1 << a.p_log2) - 1), g_id = lane_id() >> a.p_log2, h = in >> a.lh_log2;
+  const int gq_part = pass % a.gq_passes, wave_part = pass / a.gq_passes;
+  *heads_here = min(a.wave_heads, a.kv_heads - wave_part * a.wave_heads);
+  *n_q = min(GQ, a.group - gq_part * GQ);
+  const bool on = h < *heads_here;
   Place pl;
-  {
-    const int in = lane & (p_lanes - 1), h = in >> a.lh_log2;
-    const int wave_part = pass / a.gq_passes, gq_part = pass % a.gq_passes;
-    pl.col = (in & (lh - 1)) * kChunk;
-    pl.kv = wave_part * a.wave_heads + h;
-    pl.on = h < a.wave_heads && pl.kv < a.kv_heads;
-    if (!pl.on) pl.kv = 0;
-    pl.cols = min(kChunk, max(0, a.dim - pl.col));
-    pl.n_q = pl.on ? min(GQ, a.group - gq_part * GQ) : 0;
-    pl.head = pl.kv * a.group + gq_part * GQ;
-  }
-  const long long n = a.n_dev ? min(a.n_rows, max(0ll, *a.n_dev)) : a.n_rows;
-  float q[GQ][kChunk];
-  State<GQ> st;
-  auto read_q = [&](long long row, bool real) {
+  pl.sub = g_id & ((1 << r_log2) - 1);
+  pl.part = in & ((1 << a.lh_log2) - 1);
+  pl.some = on && pl.part * kChunk < a.dim;
+  pl.col = pl.some && WIDE ? min(pl.part * kChunk, a.dim - kChunk) : 0;
+  pl.kv = on ? wave_part * a.wave_heads + h : 0;
+  pl.n_q = on ? *n_q : 0;
+  pl.head = pl.kv * a.group + gq_part * GQ;
+  pl.local = h * GQ;
+  return pl;
+}
+
+template <int GQ, bool WIDE>
+__device__ __forceinline__ void read_q(const Attn& a, const Place& pl, long long row, bool real, float (&q)[GQ][kChunk]) {
 #pragma unroll
-    for (int g = 0; g < GQ; ++g) {
+  for (int g = 0; g < GQ; ++g) {
 #pragma unroll
-      for (int j = 0; j < kChunk; ++j) q[g][j] = 0.f;
-      if (real && g < pl.n_q && pl.cols > 0)
-        read_chunk(a.type, a.q + row * a.q_stride + ((long long)(pl.head + g) * a.dim + pl.col) * type_bytes(a.type), pl.cols, a.q_wide, q[g]);
+    for (int j = 0; j < kChunk; ++j) q[g][j] = 0.f;
+    if (real && g < pl.n_q && pl.some) {
+      const char* p = a.q + row * a.q_stride + ((pl.head + g) * a.dim + pl.col) * type_bytes(a.type);
+      if (WIDE) read_chunk(a.type, p, q[g]);
+      else read_chunk(a.type, p, a.dim, q[g]);
     }
-  };
-  if (chunks) {
-    const long long c = unit0 / a.passes;
-    if (c >= a.n_chunks || n == 0) return;
-    const long long c0 = c * a.chunk, c1 = min(c0 + a.chunk, min(a.n_edges, a.indptr[n]));
-    if (c0 >= c1) return;
-    pl.sub = lane >> a.p_log2;
-    const long long first = row_of(a.indptr, n, c0), last = row_of(a.indptr, n, c1 - 1);
-    for (int piece = 0; piece < 2; ++piece) {
-      const long long row = piece ? last : first;
-      if (piece && first == last) break;
-      const long long b = a.indptr[row], e = a.indptr[row + 1];
-      if (e - b <= a.chunk) continue;
-      read_q(row, true);
-      st.clear();
-      attend<TYPE, GQ, BIAS>(a, pl, max(b, c0), min(e, c1), 6 - a.p_log2, q, st);
-      for (int apart = p_lanes; apart < kWave; apart <<= 1) join_lanes<GQ>(st, apart);
-      if (lane < p_lanes && pl.cols > 0) {
 #pragma unroll
-        for (int g = 0; g < GQ; ++g) {
-          if (g < pl.n_q) {
-            const long long at = (2 * c + (b > c0 ? 1 : 0)) * a.heads + pl.head + g;
-            if (pl.col == 0) {
-              a.part_ml[2 * at] = st.m[g];
-              a.part_ml[2 * at + 1] = st.l[g];
-            }
-            float4* acc = reinterpret_cast<float4*>(a.part_acc + at * ((a.dim + kChunk - 1) / kChunk * kChunk) + pl.col);
+    for (int j = 0; j < kChunk; ++j)
+      if (WIDE && pl.col + j < pl.part * kChunk) q[g][j] = 0.f;
+  }
+}
+
+__device__ __forceinline__ long long rows_of(const Attn& a) { return a.n_dev ? min(a.n_rows, max(0ll, *a.n_dev)) : a.n_rows; }
+
+// A chunk to a wavefront: the pieces of up to two long lists, left in the workspace
+template <int TYPE, int GQ, bool BIAS, bool WIDE>
+__global__ __launch_bounds__(kAttnBlock, kWavesPerSimd<GQ>) void k_attn_chunks(const Attn a) {
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), p_lanes = 1 << a.p_log2;
+  const unsigned unit = blockIdx.x * kAttnWaves + wave, c = unit / (unsigned)a.passes;  // wavefronts side by side read the same rows
+  int heads_here, n_q;
+  const Place pl = place_of<GQ, WIDE>(a, (int)(unit - c * a.passes), 6 - a.p_log2, &heads_here, &n_q);
+  const long long n = rows_of(a);
+  if (c >= (unsigned)a.n_chunks || n == 0) return;
+  const long long c0 = (long long)c * a.chunk, c1 = min(c0 + a.chunk, min(a.n_edges, a.indptr[n]));
+  if (c0 >= c1) return;
+  const long long first = row_of(a.indptr, n, c0), last = row_of(a.indptr, n, c1 - 1);
+  for (int piece = 0; piece < (first == last ? 1 : 2); ++piece) {
+    const long long row = piece ? last : first, b = a.indptr[row], e = a.indptr[row + 1];
+    if (e - b <= a.chunk) continue;
+    float q[GQ][kChunk];
+    read_q<GQ, WIDE>(a, pl, row, true, q);
+    State<GQ> st;
+    st.clear();
+    (void)attend<TYPE, GQ, BIAS, WIDE>(a, pl, max(b, c0), min(e, c1), 6 - a.p_log2, q, st, nullptr, a.scores);
+    for (int apart = p_lanes; apart < kWave; apart <<= 1) join_lanes<GQ>(st, apart);
+    if (lane_id() < p_lanes && pl.some) {
 #pragma unroll
-            for (int j = 0; j < kChunk / 4; ++j)
-              acc[j] = make_float4(st.acc[g][4 * j], st.acc[g][4 * j + 1], st.acc[g][4 * j + 2], st.acc[g][4 * j + 3]);
+      for (int g = 0; g < GQ; ++g) {
+        if (g < pl.n_q) {
+          const long long at = (2 * (long long)c + (b > c0 ? 1 : 0)) * a.heads + pl.head + g;
+          if (pl.part == 0) {
+            a.part_ml[2 * at] = st.m[g];
+            a.part_ml[2 * at + 1] = st.l[g];
           }
+          write_chunk_as<DCI_F32>(reinterpret_cast<char*>(a.part_acc + at * ((a.dim + kChunk - 1) / kChunk * kChunk) + pl.col), kChunk, true, st.acc[g]);
         }
       }
     }
-    return;
   }
-  const int r_log2 = a.r_log2, r = 1 << r_log2, rows_at_once = groups >> r_log2;
-  const int g_id = lane >> a.p_log2;
-  pl.sub = g_id & (r - 1);
-  const long long stride = (long long)a.row_blocks * kAttnWaves / a.passes * rows_at_once;
-  for (long long row0 = unit0 / a.passes * rows_at_once; row0 < n; row0 += stride) {
-    const long long row = row0 + (g_id >> r_log2);
-    const bool real = row < n;
+}
+
+// Rows, one or more to a wavefront, one set after the other; cut lists are not its business
+template <int TYPE, int GQ, bool BIAS, bool WIDE>
+__global__ __launch_bounds__(kAttnBlock, kWavesPerSimd<GQ>) void k_attn_rows(const Attn a) {
+  extern __shared__ float stash_all[];
+  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
+  const int p_lanes = 1 << a.p_log2, groups = kWave >> a.p_log2, g_id = lane >> a.p_log2, r_log2 = a.r_log2;
+  const unsigned unit = blockIdx.x * kAttnWaves + wave, turn = unit / (unsigned)a.passes;
+  int heads_here, n_q;
+  const Place pl = place_of<GQ, WIDE>(a, (int)(unit - turn * a.passes), r_log2, &heads_here, &n_q);
+  const long long n = rows_of(a);
+  const int at_once = groups >> r_log2;
+  const unsigned turns = (unsigned)((n + at_once - 1) / at_once), step = gridDim.x * kAttnWaves / (unsigned)a.passes;
+  float* stash = stash_all + wave * (kWave + groups) * a.stash_row;
+  for (unsigned k = turn; k < turns; k += step) {
+    const long long row = (long long)k * at_once + (g_id >> r_log2);
     long long b = 0, e = 0;
-    if (real) {
-      b = max(0ll, a.indptr[row]);
-      e = min(a.n_edges, a.indptr[row + 1]);
-      if (e < b) e = b;
+    if (row < n) {
+      b = a.indptr[row];
+      e = a.indptr[row + 1];
     }
-    const bool mine = real && (a.n_chunks == 0 || e - b <= a.chunk);
+    float q[GQ][kChunk];
+    read_q<GQ, WIDE>(a, pl, row, row < n, q);
+    b = max(0ll, b);
+    e = max(b, min(a.n_edges, e));
+    const bool mine = row < n && !(a.n_chunks && e - b > a.chunk);
     if (!mine) e = b;
-    read_q(row, mine);
+    State<GQ> st;
     st.clear();
-    attend<TYPE, GQ, BIAS>(a, pl, b, e, r_log2, q, st);
-    for (int apart = p_lanes; apart < (p_lanes << r_log2); apart <<= 1) join_lanes<GQ>(st, apart);
+    // with weights: the scores of P << r_log2 entries at a time are gone through at the end, made anew if there are more
+    const long long batch = p_lanes << r_log2;
+    const bool whole = e - b <= batch;
+    const int named_all = attend<TYPE, GQ, BIAS, WIDE>(a, pl, b, e, r_log2, q, st, a.stash_row && whole ? stash : nullptr, nullptr);
+    for (int apart = p_lanes; apart < p_lanes << r_log2; apart <<= 1) join_lanes<GQ>(st, apart);
     float lse[GQ];
 #pragma unroll
     for (int g = 0; g < GQ; ++g) {
-      lse[g] = st.l[g] == 0.f ? -INFINITY : st.m[g] + logf(st.l[g]);
-      if (mine && pl.sub == 0 && g < pl.n_q) {
-        const float inv = st.l[g] == 0.f ? 0.f : 1.f / st.l[g];
+      lse[g] = st.l[g] == 0.f ? -INFINITY : st.m[g] + log_of(st.l[g]);
+      if (mine && pl.sub == 0 && g < pl.n_q && pl.some) {
+        const float inv = st.l[g] == 0.f ? 0.f : __builtin_amdgcn_rcpf(st.l[g]);
         float y[kChunk];
 #pragma unroll
         for (int j = 0; j < kChunk; ++j) y[j] = st.acc[g][j] * inv;
-        if (pl.cols > 0)
-          write_chunk(a.type, a.out + row * a.out_stride + ((long long)(pl.head + g) * a.dim + pl.col) * type_bytes(a.type), pl.cols,
-                      a.out_wide, y);
-        if (a.lse && pl.col == 0) a.lse[row * a.heads + pl.head + g] = lse[g];
+        write_chunk(a.type, a.out + row * a.out_stride + ((pl.head + g) * a.dim + pl.col) * type_bytes(a.type), WIDE ? kChunk : a.dim, WIDE, y);
+        if (a.lse && pl.part == 0) a.lse[row * a.heads + pl.head + g] = lse[g];
       }
     }
-    if (a.scores) {
-      __threadfence_block();  // the scores of this wavefront's other lanes
-      const int len = (int)(e - b);
-      for (int t0 = 0; t0 < len; t0 += r * lh) {
-        const int t = t0 + pl.sub * lh + pl.col / kChunk;
+    if (!a.stash_row) continue;
+    float* lses = stash + (kWave + g_id) * a.stash_row;
+    if (pl.part == 0) {
+#pragma unroll
+      for (int g = 0; g < GQ; ++g)
+        if (g < pl.n_q) lses[pl.local + g] = lse[g];
+    }
+    for (long long from = b; from < e; from += batch) {
+      int named_here = named_all;
+      if (!whole) {
+        State<GQ> unused;
+        unused.clear();
+        named_here = attend<TYPE, GQ, BIAS, WIDE>(a, pl, from, min(e, from + batch), r_log2, q, unused, stash, nullptr);
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      if (named_here >= 0) {  // every lane its own entry, over the wavefront's heads
+        const float* zs = stash + lane * a.stash_row;
         float p = 0.f;
-        if (t < len && pl.on) {
+        for (int h = 0; h < heads_here; ++h) {
 #pragma unroll
           for (int g = 0; g < GQ; ++g) {
-            if (g < pl.n_q) {
-              const float z = a.scores[(b + t) * a.heads + pl.head + g];
-              if (z != -INFINITY) p += exp_diff(z, lse[g]);
+            if (g < n_q) {
+              const float z = zs[h * GQ + g];
+              if (z != -INFINITY) p += exp_diff(z, lses[h * GQ + g]);
             }
           }
         }
-        for (int apart = lh; apart < p_lanes; apart <<= 1) p += __shfl_xor(p, apart, kWave);
-        if (t < len && (lane & (p_lanes - 1)) < lh) add_weight(a, a.src[b + t], p);
+        add_weight(a, named_here, p);
       }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
     }
   }
 }
 
-// One workgroup per chunk and head: the list that begins in the chunk, if it is a long one
-__global__ __launch_bounds__(kAttnBlock) void k_attn_join(const Attn a) {
+// One workgroup per row and head, or, where there are fewer of them, per chunk and head, for the long list that begins in the chunk: the list's
+// pieces added up in order.  Their weights exp(m - max) are made 256 at a time, in LDS; columns lie side by side, in as many slices of the pieces
+// as the workgroup has room for.
+__global__ __launch_bounds__(kAttnBlock) void k_attn_join(const Attn a, bool by_row) {
   const int head = (int)(blockIdx.x % (unsigned)a.heads);
-  const long long c = blockIdx.x / (unsigned)a.heads;
   const long long n = a.n_dev ? min(a.n_rows, max(0ll, *a.n_dev)) : a.n_rows;
-  if (n == 0) return;
-  const long long total = min(a.n_edges, a.indptr[n]);
-  const long long c0 = c * a.chunk, c1 = min(c0 + a.chunk, total);
-  if (c0 >= c1) return;
-  const long long row = row_of(a.indptr, n, c1 - 1);
-  const long long b = a.indptr[row], e = min(total, a.indptr[row + 1]);
-  if (b < c0 || e - b <= a.chunk) return;
+  long long row = blockIdx.x / (unsigned)a.heads;
+  if (by_row) {
+    if (row >= n) return;
+  } else {
+    if (n == 0) return;
+    const long long c0 = row * a.chunk, c1 = min(c0 + a.chunk, min(a.n_edges, a.indptr[n]));
+    if (c0 >= c1) return;
+    row = row_of(a.indptr, n, c1 - 1);
+    if (a.indptr[row] < c0) return;
+  }
+  const long long b = a.indptr[row], e = min(a.n_edges, a.indptr[row + 1]);
+  if (b < 0 || e - b <= a.chunk) return;
+  const long long c = b / a.chunk;
   const int width = (a.dim + kChunk - 1) / kChunk * kChunk;
   const int pieces = (int)((e - 1) / a.chunk - c) + 1;
-  auto place = [&](int k) { return (2 * (c + k) + (k == 0 && b != c0 ? 1 : 0)) * a.heads + head; };
-  __shared__ float part[kAttnBlock], red[kAttnWaves];
+  auto place = [&](int k) { return (2 * (c + k) + (k == 0 && b != c * a.chunk ? 1 : 0)) * a.heads + head; };
+  __shared__ float part[kAttnBlock], red[kAttnWaves], weights[kAttnBlock];
   const int lane = lane_id(), wave = (int)threadIdx.x / kWave;
   float m = -INFINITY;
   for (int k = (int)threadIdx.x; k < pieces; k += kAttnBlock) m = fmaxf(m, a.part_ml[2 * place(k)]);
@@ -408,32 +467,36 @@ __global__ __launch_bounds__(kAttnBlock) void k_attn_join(const Attn a) {
   __syncthreads();
 #pragma unroll
   for (int w = 0; w < kAttnWaves; ++w) m = fmaxf(m, red[w]);
-  const float base = finite_or_0(m);
-  __syncthreads();
-  float l = 0.f;
-  for (int k = (int)threadIdx.x; k < pieces; k += kAttnBlock) {
-    const long long at = place(k);
-    l += a.part_ml[2 * at + 1] * exp_diff(a.part_ml[2 * at], base);
+  const float top = finite_or_0(m);
+  int cols = 16;
+  while (cols < width) cols <<= 1;
+  const int slices = kAttnBlock / cols, col = (int)threadIdx.x & (cols - 1), slice = (int)threadIdx.x / cols;
+  float acc = 0.f, l = 0.f;
+  for (int k0 = 0; k0 < pieces; k0 += kAttnBlock) {
+    const int k = k0 + (int)threadIdx.x;
+    float w = 0.f;
+    if (k < pieces) {
+      const long long at = place(k);
+      w = exp_diff(a.part_ml[2 * at], top);
+      l += a.part_ml[2 * at + 1] * w;
+    }
+    __syncthreads();
+    weights[threadIdx.x] = w;
+    __syncthreads();
+    if (col < width) {
+      const int end = min(kAttnBlock, pieces - k0);
+#pragma unroll 8
+      for (int i = slice; i < end; i += slices) acc = fmaf(a.part_acc[place(k0 + i) * width + col], weights[i], acc);
+    }
   }
   for (int d = kWave / 2; d; d >>= 1) l += __shfl_xor(l, d, kWave);
+  __syncthreads();
   if (lane == 0) red[wave] = l;
+  part[threadIdx.x] = acc;
   __syncthreads();
   l = 0.f;
 #pragma unroll
   for (int w = 0; w < kAttnWaves; ++w) l += red[w];
-  // columns side by side, as many slices of the pieces as the workgroup has room for
-  int cols = 16;
-  while (cols < width) cols <<= 1;
-  const int slices = kAttnBlock / cols, col = (int)threadIdx.x & (cols - 1), slice = (int)threadIdx.x / cols;
-  float acc = 0.f;
-  if (col < width) {
-    for (int k = slice; k < pieces; k += slices) {
-      const long long at = place(k);
-      acc += a.part_acc[at * width + col] * exp_diff(a.part_ml[2 * at], base);
-    }
-  }
-  part[threadIdx.x] = acc;
-  __syncthreads();
   if (slice == 0 && col < a.dim) {
     for (int s = 1; s < slices; ++s) acc += part[s * cols + col];
     const float y = l == 0.f ? 0.f : acc / l;
@@ -443,7 +506,7 @@ __global__ __launch_bounds__(kAttnBlock) void k_attn_join(const Attn a) {
     else *reinterpret_cast<unsigned short*>(o) = (unsigned short)two<DCI_F16>(y, 0.f);
   }
   if (threadIdx.x == 0) {
-    const float lse = l == 0.f ? -INFINITY : m + logf(l);
+    const float lse = l == 0.f ? -INFINITY : m + log_of(l);
     if (a.lse) a.lse[row * a.heads + head] = lse;
     if (a.all_lse) a.all_lse[row * a.heads + head] = lse;
   }
@@ -469,7 +532,7 @@ __global__ __launch_bounds__(kAttnBlock) void k_attn_weights(const Attn a) {
         const float z = a.scores[t * a.heads + h];
         if (z != -INFINITY) p += exp_diff(z, a.all_lse[row * a.heads + h]);
       }
-      add_weight(a, a.src[t], p);
+      add_weight(a, named(a, a.src[t]), p);
     }
   }
 }
@@ -478,21 +541,27 @@ __global__ __launch_bounds__(kAttnBlock) void k_attn_weights(const Attn a) {
 // How a call's work is cut, from its arguments alone (the workspace query has no context)
 struct Split {
   int p_log2, lh_log2, wave_heads, gq, gq_passes, passes;
+  bool wide;  // heads of 16 columns at least: read and written 16 at a time
   int chunk;
   int64_t n_chunks;
 };
 constexpr int64_t kWantedWaves = 4096;  // 16 to a compute unit
+constexpr int kStashHeads = 32;  // query heads of a wavefront, at most, with weights: 40 KB of scores to a workgroup, four workgroups to a compute unit
 
-Split split_of(const dci_attn& t) {
+Split split_of(const dci_attn& t, bool accumulate) {
   Split s;
+  s.wide = t.head_dim >= kChunk;
+  const int group = t.n_heads / t.kv_heads, gq = group == 1 || !s.wide ? 1 : group == 2 ? 2 : 4;
   s.lh_log2 = log2_up((t.head_dim + kChunk - 1) / kChunk);
-  s.p_log2 = log2_up((int64_t)t.kv_heads << s.lh_log2);
-  if (s.p_log2 > 6) s.p_log2 = 6;
-  s.wave_heads = (kWave >> s.lh_log2) < t.kv_heads ? (kWave >> s.lh_log2) : t.kv_heads;
-  const int group = t.n_heads / t.kv_heads;
-  s.gq = group == 1 ? 1 : group == 2 ? 2 : 4;
+  s.wave_heads = kWave >> s.lh_log2;
+  if (accumulate && s.wave_heads > kStashHeads / gq) s.wave_heads = kStashHeads / gq;
+  if (s.wave_heads > t.kv_heads) s.wave_heads = t.kv_heads;
+  s.p_log2 = log2_up((int64_t)s.wave_heads << s.lh_log2);
+  if (s.p_log2 < 2) s.p_log2 = 2;  // entries are taken four at a time
+  const int parts = (t.kv_heads + s.wave_heads - 1) / s.wave_heads;
+  s.gq = gq;
   s.gq_passes = (group + s.gq - 1) / s.gq;
-  s.passes = (t.kv_heads + s.wave_heads - 1) / s.wave_heads * s.gq_passes;
+  s.passes = parts * s.gq_passes;
   // chunks of 64 to 512 entries: as long as there are wavefronts enough
   s.chunk = 64;
   while (s.chunk < 512 && t.n_edges / s.chunk * s.passes > kWantedWaves) s.chunk *= 2;
@@ -506,8 +575,8 @@ struct Parts {
 };
 Parts take_parts(Arena& ar, const dci_attn& t, const Split& s, bool accumulate) {
   Parts p;
-  if (accumulate) p.scores = ar.take<float>((size_t)t.n_edges * t.n_heads);
   if (s.n_chunks) {
+    if (accumulate) p.scores = ar.take<float>((size_t)t.n_edges * t.n_heads);
     if (accumulate) p.all_lse = ar.take<float>((size_t)t.n_rows * t.n_heads);
     p.ml = ar.take<float>((size_t)s.n_chunks * 2 * t.n_heads * 2);
     p.acc = ar.take<float>((size_t)s.n_chunks * 2 * t.n_heads * kv_width(t.head_dim));
@@ -548,28 +617,34 @@ int32_t check_attn(dci_ctx* ctx, const dci_attn* t) {
   return DCI_OK;
 }
 
+// n_chunks wavefronts' worth of chunks, if there are any, and the rows
+template <int TYPE, int GQ, bool BIAS, bool WIDE>
+void launch_attn(const Attn& a, unsigned chunk_grid, unsigned row_grid, unsigned lds, hipStream_t stream) {
+  if (chunk_grid) hipLaunchKernelGGL((k_attn_chunks<TYPE, GQ, BIAS, WIDE>), dim3(chunk_grid), dim3(kAttnBlock), 0, stream, a);
+  hipLaunchKernelGGL((k_attn_rows<TYPE, GQ, BIAS, WIDE>), dim3(row_grid), dim3(kAttnBlock), lds, stream, a);
+}
+template <int TYPE, int GQ, bool WIDE>
+void launch_attn(const Attn& a, unsigned chunk_grid, unsigned row_grid, unsigned lds, hipStream_t stream) {
+  if (a.bias) launch_attn<TYPE, GQ, true, WIDE>(a, chunk_grid, row_grid, lds, stream);
+  else launch_attn<TYPE, GQ, false, WIDE>(a, chunk_grid, row_grid, lds, stream);
+}
 template <int TYPE>
-void launch_attn(int gq, const Attn& a, dim3 grid, hipStream_t stream) {
-#define DCI_ATTN(GQ_)                                                                                             \
-  do {                                                                                                            \
-    if (a.bias) hipLaunchKernelGGL((k_attn<TYPE, GQ_, true>), grid, dim3(kAttnBlock), 0, stream, a);              \
-    else hipLaunchKernelGGL((k_attn<TYPE, GQ_, false>), grid, dim3(kAttnBlock), 0, stream, a);                    \
-  } while (0)
-  if (gq == 1) DCI_ATTN(1);
-  else if (gq == 2) DCI_ATTN(2);
-  else DCI_ATTN(4);
-#undef DCI_ATTN
+void launch_attn(const Split& s, const Attn& a, unsigned chunk_grid, unsigned row_grid, unsigned lds, hipStream_t stream) {
+  if (!s.wide) launch_attn<TYPE, 1, false>(a, chunk_grid, row_grid, lds, stream);
+  else if (s.gq == 1) launch_attn<TYPE, 1, true>(a, chunk_grid, row_grid, lds, stream);
+  else if (s.gq == 2) launch_attn<TYPE, 2, true>(a, chunk_grid, row_grid, lds, stream);
+  else launch_attn<TYPE, 4, true>(a, chunk_grid, row_grid, lds, stream);
 }
 
 int32_t attn(dci_ctx* ctx, const dci_attn& t, int type, Attn a, bool accumulate) {
-  const Split s = split_of(t);
+  const Split s = split_of(t, accumulate);
   Arena ar(ctx->ws, ctx->ws_bytes);
   const Parts parts = take_parts(ar, t, s, accumulate);
   if (!ar.ok()) {
     ctx->req_workspace = ar.off;
     return fail(ctx, DCI_ERR_CAPACITY, "workspace holds %zu bytes, this attention call needs %zu", ctx->ws_bytes, ar.off);
   }
-  if (s.n_chunks * t.n_heads > 0x7FFFFFFFll || s.n_chunks * s.passes > 0x7FFFFFFFll)
+  if (s.n_chunks * t.n_heads > 0x7FFFFFFFll || s.n_chunks * s.passes > 0x7FFFFFFFll || t.n_rows * s.passes > 0xF0000000ll)
     return fail(ctx, DCI_ERR_UNSUPPORTED, "attention: too many list entries and heads for one call");
   const int64_t b = type_bytes(t.dtype);
   a.n_rows = t.n_rows;
@@ -587,11 +662,12 @@ int32_t attn(dci_ctx* ctx, const dci_attn& t, int type, Attn a, bool accumulate)
   a.out = static_cast<char*>(t.out);
   a.q_stride = t.q_stride * b;
   a.out_stride = t.out_stride * b;
-  a.q_wide = by_16_bytes(t.q, t.q_stride, t.head_dim, t.dtype);
-  a.out_wide = by_16_bytes(t.out, t.out_stride, t.head_dim, t.dtype);
   a.lse = t.lse;
   a.bias = t.bias;
   a.bias_heads = t.bias_heads;
+  // with weights, LDS for 64 entries' scores and a row of lse to each lane group
+  a.stash_row = accumulate && t.n_edges > 0 ? (s.wave_heads * s.gq) | 1 : 0;
+  const unsigned lds = (unsigned)(kAttnWaves * (kWave + (kWave >> s.p_log2)) * a.stash_row * sizeof(float));
   a.scores = parts.scores;
   a.all_lse = parts.all_lse;
   a.part_ml = parts.ml;
@@ -603,29 +679,31 @@ int32_t attn(dci_ctx* ctx, const dci_attn& t, int type, Attn a, bool accumulate)
   a.gq_passes = s.gq_passes;
   a.chunk = s.chunk;
   a.n_chunks = (int)s.n_chunks;
-  a.chunk_blocks = (int)((s.n_chunks * s.passes + kAttnWaves - 1) / kAttnWaves);
-  // lane groups to a row: one, unless that leaves wavefronts to be had; no more than there are entries in a list
+  // lane groups to a row: one, unless that leaves wavefronts to be had (no more then than there are entries in a list) or, with weights, the scores
+  // of the longest list would not all be at hand at its end
   const int groups_log2 = 6 - s.p_log2;
-  const int64_t mean = t.n_edges / t.n_rows;
+  const int64_t mean = t.n_edges / t.n_rows, longest = s.n_chunks ? s.chunk : t.max_list > 0 ? t.max_list : t.n_edges;
   a.r_log2 = 0;
-  while (a.r_log2 < groups_log2 && ((t.n_rows * s.passes) << a.r_log2 >> groups_log2) < kWantedWaves && (2ll << a.r_log2) <= mean) ++a.r_log2;
+  while (a.r_log2 < groups_log2 && ((((t.n_rows * s.passes) << a.r_log2 >> groups_log2) < kWantedWaves && (2ll << a.r_log2) <= mean) ||
+                                    (accumulate && (1ll << (s.p_log2 + a.r_log2)) < longest)))
+    ++a.r_log2;
   const int64_t at_once = 1ll << (groups_log2 - a.r_log2);
   int64_t blocks = ((t.n_rows + at_once - 1) / at_once * s.passes + kAttnWaves - 1) / kAttnWaves;
   if (blocks > (int64_t)ctx->num_cus * 32) blocks = (int64_t)ctx->num_cus * 32;
   blocks = (blocks + s.passes - 1) / s.passes * s.passes;  // a wavefront keeps its share of the heads from row to row
-  a.row_blocks = (int)blocks;
+  const unsigned chunk_grid = (unsigned)((s.n_chunks * s.passes + kAttnWaves - 1) / kAttnWaves), row_grid = (unsigned)blocks;
   const OnDevice on(ctx->device);
   DCI_HIP(ctx, on.err);
   {
     Timed timed(ctx, DCI_K_ATTN);
-    const dim3 grid((unsigned)(a.chunk_blocks + a.row_blocks));
-    if (type == kE4M3) launch_attn<kE4M3>(s.gq, a, grid, ctx->stream);
-    else if (type == DCI_F32) launch_attn<DCI_F32>(s.gq, a, grid, ctx->stream);
-    else if (type == DCI_BF16) launch_attn<DCI_BF16>(s.gq, a, grid, ctx->stream);
-    else launch_attn<DCI_F16>(s.gq, a, grid, ctx->stream);
+    if (type == kE4M3) launch_attn<kE4M3>(s, a, chunk_grid, row_grid, lds, ctx->stream);
+    else if (type == DCI_F32) launch_attn<DCI_F32>(s, a, chunk_grid, row_grid, lds, ctx->stream);
+    else if (type == DCI_BF16) launch_attn<DCI_BF16>(s, a, chunk_grid, row_grid, lds, ctx->stream);
+    else launch_attn<DCI_F16>(s, a, chunk_grid, row_grid, lds, ctx->stream);
     DCI_LAUNCH_CHECK(ctx);
     if (s.n_chunks) {
-      hipLaunchKernelGGL(k_attn_join, dim3((unsigned)(s.n_chunks * t.n_heads)), dim3(kAttnBlock), 0, ctx->stream, a);
+      const bool by_row = t.n_rows <= s.n_chunks;
+      hipLaunchKernelGGL(k_attn_join, dim3((unsigned)((by_row ? t.n_rows : s.n_chunks) * t.n_heads)), dim3(kAttnBlock), 0, ctx->stream, a, by_row);
       DCI_LAUNCH_CHECK(ctx);
       if (accumulate) {
         hipLaunchKernelGGL(k_attn_weights, dim3((unsigned)((s.n_chunks + kAttnWaves - 1) / kAttnWaves)), dim3(kAttnBlock), 0, ctx->stream, a);
@@ -644,7 +722,7 @@ extern "C" {
 size_t dci_attn_workspace_bytes(const dci_attn* attn, int32_t accumulate) {
   if (!attn || !dci::sizes_ok(*attn) || attn->n_edges > dci::kMaxEdges) return 0;
   dci::Arena ar(nullptr, 0);
-  (void)dci::take_parts(ar, *attn, dci::split_of(*attn), accumulate != 0);
+  (void)dci::take_parts(ar, *attn, dci::split_of(*attn, accumulate != 0), accumulate != 0);
   return ar.off;
 }
 
@@ -655,6 +733,7 @@ int32_t dci_attn_forward(dci_ctx* ctx, const dci_attn* attn, const void* k, int6
   if (k_stride < row || v_stride < row)
     return dci::fail(ctx, DCI_ERR_INVALID_ARG, "attention: k and v rows are kv_heads * head_dim = %lld numbers long, strides %lld and %lld",
                      (long long)row, (long long)k_stride, (long long)v_stride);
+  if (k_stride >= 1ll << 30 || v_stride >= 1ll << 30) return dci::fail(ctx, DCI_ERR_UNSUPPORTED, "attention: k and v strides of 2^30 numbers and more");
   if (attn->n_src > 0 && (!k || !v)) return dci::fail(ctx, DCI_ERR_INVALID_ARG, "attention: null k or v");
   if (!dci::aligned_rows(k, attn->dtype) || !dci::aligned_rows(v, attn->dtype))
     return dci::fail(ctx, DCI_ERR_INVALID_ARG, "attention: k and v must be aligned to their type");
@@ -663,9 +742,8 @@ int32_t dci_attn_forward(dci_ctx* ctx, const dci_attn* attn, const void* k, int6
   a.n_src = a.n_at = (unsigned)attn->n_src;
   a.k = static_cast<const char*>(k);
   a.v = static_cast<const char*>(v);
-  a.k_stride = k_stride * dci::type_bytes(attn->dtype);
-  a.v_stride = v_stride * dci::type_bytes(attn->dtype);
-  a.kv_wide = dci::by_16_bytes(k, k_stride, attn->head_dim, attn->dtype) && dci::by_16_bytes(v, v_stride, attn->head_dim, attn->dtype);
+  a.k_stride = (unsigned)(k_stride * dci::type_bytes(attn->dtype));
+  a.v_stride = (unsigned)(v_stride * dci::type_bytes(attn->dtype));
   return dci::attn(ctx, *attn, attn->dtype, a, false);
 }
 
@@ -685,8 +763,7 @@ int32_t dci_attn_cached(dci_ctx* ctx, const dci_attn* attn, const dci_kv_cache* 
   a.n_src = slots ? (unsigned)attn->n_src : a.n_at;
   a.k = reinterpret_cast<const char*>(cache->codes);
   a.v = a.k + (int64_t)cache->kv_heads * width;
-  a.k_stride = a.v_stride = 2ll * cache->kv_heads * width;
-  a.kv_wide = true;
+  a.k_stride = a.v_stride = 2u * cache->kv_heads * width;
   a.scales = cache->scales;
   a.block_log2 = dci::log2_up(cache->block);
   a.weight = reinterpret_cast<unsigned long long*>(cache->weight);

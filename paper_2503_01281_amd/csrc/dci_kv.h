@@ -43,6 +43,17 @@ struct OnDevice {
 
 int32_t check_kv_cache(dci_ctx* ctx, const dci_kv_cache* cache);
 
+// Sixteen bytes anywhere: the loads and stores of rows need no alignment beyond their type's.
+typedef unsigned u32x4_any __attribute__((ext_vector_type(4), aligned(1)));
+__device__ __forceinline__ uint4 load_16(const char* p) {
+  const u32x4_any v = *reinterpret_cast<const u32x4_any*>(p);
+  return make_uint4(v.x, v.y, v.z, v.w);
+}
+__device__ __forceinline__ void store_16(char* p, uint4 v) {
+  const u32x4_any u = {v.x, v.y, v.z, v.w};
+  *reinterpret_cast<u32x4_any*>(p) = u;
+}
+
 // 16 columns of a row as they lie in memory.
 template <int TYPE>
 struct Chunk {
@@ -52,6 +63,10 @@ struct Chunk {
   __device__ __forceinline__ void clear() {
 #pragma unroll
     for (int j = 0; j < kWords; ++j) w[j] = make_uint4(0, 0, 0, 0);
+  }
+  __device__ __forceinline__ void load(const char* p) {
+#pragma unroll
+    for (int j = 0; j < kWords; ++j) w[j] = load_16(p + 16 * j);
   }
   // The first `cols` (1 .. 16) of them from p, the others 0; wide: by 16 bytes (by_16_bytes), else number by number.
   __device__ __forceinline__ void load(const char* p, int cols, bool wide) {
@@ -102,7 +117,7 @@ struct Chunk {
   }
 };
 
-// 16 columns from p as numbers, whatever their type
+// 16 columns from p as numbers
 template <int TYPE>
 __device__ __forceinline__ void read_chunk_as(const char* p, int cols, bool wide, float (&x)[kChunk]) {
   Chunk<TYPE> c;
@@ -110,10 +125,30 @@ __device__ __forceinline__ void read_chunk_as(const char* p, int cols, bool wide
 #pragma unroll
   for (int j = 0; j < kChunk / 2; ++j) c.pair(j, x[2 * j], x[2 * j + 1]);
 }
-__device__ __forceinline__ void read_chunk(int type, const char* p, int cols, bool wide, float (&x)[kChunk]) {
-  if (type == DCI_F32) read_chunk_as<DCI_F32>(p, cols, wide, x);
-  else if (type == DCI_BF16) read_chunk_as<DCI_BF16>(p, cols, wide, x);
-  else read_chunk_as<DCI_F16>(p, cols, wide, x);
+// Whatever their type, all 16 or the first `cols`
+__device__ __forceinline__ void read_chunk(int type, const char* p, float (&x)[kChunk]) {
+  Chunk<DCI_F32> c;
+  if (type == DCI_F32) {
+    c.load(p);
+#pragma unroll
+    for (int j = 0; j < kChunk / 2; ++j) c.pair(j, x[2 * j], x[2 * j + 1]);
+  } else {
+    Chunk<DCI_BF16> b;
+    Chunk<DCI_F16> h;
+    b.load(p);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) h.w[j] = b.w[j];
+#pragma unroll
+    for (int j = 0; j < kChunk / 2; ++j) {
+      if (type == DCI_BF16) b.pair(j, x[2 * j], x[2 * j + 1]);
+      else h.pair(j, x[2 * j], x[2 * j + 1]);
+    }
+  }
+}
+__device__ __forceinline__ void read_chunk(int type, const char* p, int cols, float (&x)[kChunk]) {
+  if (type == DCI_F32) read_chunk_as<DCI_F32>(p, cols, false, x);
+  else if (type == DCI_BF16) read_chunk_as<DCI_BF16>(p, cols, false, x);
+  else read_chunk_as<DCI_F16>(p, cols, false, x);
 }
 
 template <int TYPE>
@@ -140,7 +175,7 @@ __device__ __forceinline__ void write_chunk_as(char* p, int cols, bool wide, con
   if (wide) {
 #pragma unroll
     for (int j = 0; j < type_bytes(TYPE); ++j)
-      if (j * kPer < cols) reinterpret_cast<uint4*>(p)[j] = make_uint4(u[4 * j], u[4 * j + 1], u[4 * j + 2], u[4 * j + 3]);
+      if (j * kPer < cols) store_16(p + 16 * j, make_uint4(u[4 * j], u[4 * j + 1], u[4 * j + 2], u[4 * j + 3]));
   } else {
 #pragma unroll
     for (int j = 0; j < kChunk; ++j) {
@@ -162,15 +197,20 @@ template <int CTRL>
 __device__ __forceinline__ float dpp(float x) {
   return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xF, 0xF, true));
 }
-// Sum over groups of 1 << log2 lanes (log2 <= 4), in all of them
-__device__ __forceinline__ float sum_lanes(float x, int log2) {
-  if (log2 > 0) x += dpp<0xB1>(x);   // quad_perm 1 0 3 2
-  if (log2 > 1) x += dpp<0x4E>(x);   // quad_perm 2 3 0 1
-  if (log2 > 2) x += dpp<0x141>(x);  // the other half of eight, mirrored
-  if (log2 > 3) x += dpp<0x140>(x);  // the other half of sixteen, mirrored
-  return x;
+// Sums of N numbers each over groups of 1 << log2 lanes (log2 <= 4), in all of the lanes
+template <int N>
+__device__ __forceinline__ void sum_lanes(float* x, int log2) {
+#define DCI_STEP(STEP_, CTRL_)                              \
+  if (log2 > STEP_) {                                       \
+    _Pragma("unroll") for (int i = 0; i < N; ++i) x[i] += dpp<CTRL_>(x[i]); \
+  }
+  DCI_STEP(0, 0xB1)   // quad_perm 1 0 3 2
+  DCI_STEP(1, 0x4E)   // quad_perm 2 3 0 1
+  DCI_STEP(2, 0x141)  // the other half of eight, mirrored
+  DCI_STEP(3, 0x140)  // the other half of sixteen, mirrored
+#undef DCI_STEP
 }
-// The same for the maximum
+// The maximum likewise
 __device__ __forceinline__ float max_lanes(float x, int log2) {
   if (log2 > 0) x = fmaxf(x, dpp<0xB1>(x));
   if (log2 > 1) x = fmaxf(x, dpp<0x4E>(x));

@@ -37,12 +37,11 @@ def test_workspace_sizes(lib):
         return lib.dci_attn_workspace_bytes(C.byref(a), accumulate)
 
     up = lambda x: -(-x // 256) * 256
-    assert need() == 0                                     # short lists need none
-    assert need(1) == up(1500 * 4 * 4)                     # a score per entry and head
+    assert need() == need(1) == 0                          # short lists need none
     chunks = -(-1500 // 64)
     parts = up(chunks * 2 * 4 * 2 * 4) + up(chunks * 2 * 4 * 64 * 4)
     assert need(max_list=0) == need(max_list=65) == parts  # lists that may be longer than 64
-    assert need(1, max_list=0) == parts + up(1500 * 4 * 4) + up(100 * 4 * 4)
+    assert need(1, max_list=0) == parts + up(1500 * 4 * 4) + up(100 * 4 * 4)  # a score per entry and head, a sum per row and head
     assert need(n_edges=0, max_list=0) == 0
     for bad in (dict(n_rows=-1), dict(n_heads=3), dict(kv_heads=0), dict(head_dim=0), dict(head_dim=300), dict(n_edges=2 ** 40)):
         assert need(1, **bad) == 0
