@@ -3,8 +3,9 @@
 // For a row i and a head h, over the entries e of the row's list:  z_e = scale (q_i . K_e) + bias_e,  out = sum exp(z_e) V_e / sum exp(z_e).
 // One pass over the list: a running maximum m, the sum l of exp(z - m) and the accumulator of exp(z - m) V, the last two rescaled
 // when m grows.  Every K and V row that an entry names is read once, straight into registers, 16 columns to a lane:
-//   a head's columns lie in LH = 1 .. 16 adjacent lanes (the last lane takes the head's last 16 columns, whichever of them the lane before has as
-//   well: those count once in a score, and are written twice alike), the heads of a row side by side, P lanes in all (a power of two up to 64; more
+//   a head's columns lie in LH = 1 .. 16 adjacent lanes, in pieces of 16 bytes that follow each other from lane to lane (a lane has one of an 8-bit
+//   row, two of a 16-bit, four of a 32-bit one; the piece that a head ends in is its last 16 bytes, whichever of them the piece before has as well:
+//   those count once in a score, and are written twice alike), the heads of a row side by side, P lanes in all (a power of two up to 64; more
 //   heads are shared out between wavefronts).  A score is a sum over LH lanes (DPP), and the lanes of a head then hold what they need
 //   for their columns of the output: nothing passes through LDS.
 //   The 64 / P groups of lanes of a wavefront work on rows of their own, or R of them on one row, each on every R-th entry, and join their
@@ -28,7 +29,7 @@ constexpr int kAttnBlock = 256, kAttnWaves = kAttnBlock / kWave;
 constexpr float kLog2E = 1.44269504088896340736f;
 // wavefronts to a SIMD that the registers are shared out for
 template <int GQ>
-constexpr int kWavesPerSimd = GQ == 4 ? 2 : GQ == 2 ? 3 : 4;
+constexpr int kWavesPerSimd = GQ == 4 ? 2 : 3;
 constexpr double kWeightUnit = 4294967296.0;  // 2^32
 
 struct Attn {
@@ -70,8 +71,7 @@ struct Attn {
 struct Place {
   int sub;    // its group's number among those of a row
   int part;   // its number among the head's lanes
-  int col;    // its first column: 16 * part, but that a head's last 16 columns, where they overlap those of the lane before, are its last lane's
-  bool some;  // whether there are columns for it
+  bool on;    // whether there is a head for it
   int kv;     // its key head
   int head;   // its first query head
   int n_q;    // how many query heads
@@ -118,24 +118,60 @@ __device__ __forceinline__ int named(const Attn& a, int s) {
   return in && (unsigned)at < a.n_at ? at : -1;
 }
 
-// Entries [e0, e1) of one row into st: those of group `sub` are every (1 << r_log2)-th from e0 + sub on.  Returns what the lane's entry of the last
+// The columns of a lane: piece j, kPiece<TYPE> columns from first_column on, if there are any left for it (then `some`); all of them where
+// heads are too narrow for a piece (!WIDE)
+template <int TYPE>
+constexpr int kPiece = 16 / type_bytes(TYPE);
+template <int TYPE, bool WIDE>
+__device__ __forceinline__ int first_column(const Attn& a, const Place& pl, int j, bool* some, int* skip) {
+  if (!WIDE) {
+    *some = pl.part == 0 && j == 0;
+    *skip = 0;
+    return 0;
+  }
+  const int c = ((j << a.lh_log2) + pl.part) * kPiece<TYPE>, col = min(c, a.dim - kPiece<TYPE>);
+  *some = c < a.dim;
+  *skip = c - col;  // columns that are another piece's
+  return col;
+}
+
+// Entries [e0, e1) that are gone through: none where nothing can be named
+__device__ __forceinline__ int entries(const Attn& a, long long e0, long long e1) {
+  return a.n_at > 0 && a.n_src > 0 ? (int)max(0ll, min(e1 - e0, 0x7FFFFFFFll - 8192)) : 0;
+}
+// The source of a lane's first entry of them
+__device__ __forceinline__ int first_source(const Attn& a, const Place& pl, long long e0, long long e1, int r_log2) {
+  const int t = ((lane_id() & ((1 << a.p_log2) - 1)) << r_log2) + pl.sub;
+  return t < entries(a, e0, e1) ? a.src[e0 + t] : -1;
+}
+
+// Entries [e0, e1) of one row into st (source0: their first_source): those of group `sub` are every (1 << r_log2)-th from e0 + sub on.  Returns what the lane's entry of the last
 // P << r_log2 named (there are no more where that is used).  stash (nullable): LDS for the scores, entry by entry of the wavefront; scores (nullable):
 // memory for them, entry by entry of the call.
 template <int TYPE, int GQ, bool BIAS, bool WIDE>
-__device__ __forceinline__ int attend(const Attn& a, const Place& pl, long long e0, long long e1, int r_log2, const float (&q)[GQ][kChunk],
+__device__ __forceinline__ int attend(const Attn& a, const Place& pl, long long e0, long long e1, int r_log2, int source0, const float (&q)[GQ][kChunk],
                                       State<GQ>& st, float* stash, float* scores) {
   constexpr int U = TYPE == kE4M3 ? 4 : !WIDE ? 1 : TYPE == DCI_F32 ? 2 : 4;  // entries at a time
-  const bool any = a.n_at > 0 && a.n_src > 0;  // else no entry names anything
-  const int n = any ? (int)max(0ll, min(e1 - e0, 0x7FFFFFFFll - 8192)) : 0;
+  const int n = entries(a, e0, e1);
   const int* __restrict__ src = a.src + e0;
   const int lane = lane_id(), in = lane & ((1 << a.p_log2) - 1), base = lane - in;
   const int batch = 1 << (a.p_log2 + r_log2), first = (in << r_log2) + pl.sub;
   auto source = [&](int t) { return t < n ? src[t] : -1; };
-  int next = source(first), after = source(first + batch);
-  if (n > 0) next = named(a, next);
+  int next = -1, after = source(first + batch);
+  if (n > 0) next = named(a, source0);
   const int width = TYPE == kE4M3 ? (a.dim + kChunk - 1) / kChunk * kChunk : a.dim;
-  const unsigned offset = (unsigned)(pl.kv * width + pl.col) * type_bytes(TYPE);
-  const char *k0 = a.k + offset, *v0 = a.v + offset;
+  const char *k0 = a.k + (long long)(pl.kv * width) * type_bytes(TYPE), *v0 = a.v + (long long)(pl.kv * width) * type_bytes(TYPE);
+  int offset[Chunk<TYPE>::kWords];
+#pragma unroll
+  for (int j = 0; j < Chunk<TYPE>::kWords; ++j) {
+    bool some;
+    int skip;
+    offset[j] = first_column<TYPE, WIDE>(a, pl, j, &some, &skip) * type_bytes(TYPE);
+  }
+  if (Chunk<TYPE>::kWords == 1) {
+    k0 += offset[0];
+    v0 += offset[0];
+  }
   const char* s0 = reinterpret_cast<const char*>(a.scales + 2 * pl.kv);
   const unsigned s_stride = 8u * a.kv_heads;
   int now = -1;
@@ -154,12 +190,18 @@ __device__ __forceinline__ int attend(const Attn& a, const Place& pl, long long 
         there[u] = at >= 0;
         const unsigned row = there[u] ? (unsigned)at : 0u;
         ks[u] = vs[u] = 1.f;
-        if (WIDE || TYPE == kE4M3) {
-          kc[u].load(k0 + (unsigned long long)row * a.k_stride);
-          vc[u].load(v0 + (unsigned long long)row * a.v_stride);
+        const char *pk = k0 + (unsigned long long)row * a.k_stride, *pv = v0 + (unsigned long long)row * a.v_stride;
+        if (TYPE == kE4M3) {
+          kc[u].load(pk);
+          vc[u].load(pv);
+        } else if (WIDE) {
+#pragma unroll
+          for (int j = 0; j < Chunk<TYPE>::kWords; ++j) kc[u].w[j] = load_16(pk + offset[j]);
+#pragma unroll
+          for (int j = 0; j < Chunk<TYPE>::kWords; ++j) vc[u].w[j] = load_16(pv + offset[j]);
         } else {
-          kc[u].load(k0 + (unsigned long long)row * a.k_stride, a.dim, false);
-          vc[u].load(v0 + (unsigned long long)row * a.v_stride, a.dim, false);
+          kc[u].load(pk, a.dim, false);
+          vc[u].load(pv, a.dim, false);
         }
         if (TYPE == kE4M3) {
           const float2 s = *reinterpret_cast<const float2*>(s0 + (unsigned long long)(row >> a.block_log2) * s_stride);
@@ -279,39 +321,78 @@ __device__ __forceinline__ void add_weight(const Attn& a, int at, float p) {
 }
 
 // What a lane is there for in pass `pass` over the heads
-template <int GQ, bool WIDE>
+template <int GQ>
 __device__ __forceinline__ Place place_of(const Attn& a, int pass, int r_log2, int* heads_here, int* n_q) {
   const int in = lane_id() & ((1 << a.p_log2) - 1), g_id = lane_id() >> a.p_log2, h = in >> a.lh_log2;
   const int gq_part = pass % a.gq_passes, wave_part = pass / a.gq_passes;
   *heads_here = min(a.wave_heads, a.kv_heads - wave_part * a.wave_heads);
   *n_q = min(GQ, a.group - gq_part * GQ);
-  const bool on = h < *heads_here;
   Place pl;
+  pl.on = h < *heads_here;
   pl.sub = g_id & ((1 << r_log2) - 1);
   pl.part = in & ((1 << a.lh_log2) - 1);
-  pl.some = on && pl.part * kChunk < a.dim;
-  pl.col = pl.some && WIDE ? min(pl.part * kChunk, a.dim - kChunk) : 0;
-  pl.kv = on ? wave_part * a.wave_heads + h : 0;
-  pl.n_q = on ? *n_q : 0;
+  pl.kv = pl.on ? wave_part * a.wave_heads + h : 0;
+  pl.n_q = pl.on ? *n_q : 0;
   pl.head = pl.kv * a.group + gq_part * GQ;
   pl.local = h * GQ;
   return pl;
 }
 
-template <int GQ, bool WIDE>
+template <int TYPE, int GQ, bool WIDE>
 __device__ __forceinline__ void read_q(const Attn& a, const Place& pl, long long row, bool real, float (&q)[GQ][kChunk]) {
 #pragma unroll
   for (int g = 0; g < GQ; ++g) {
+    const char* p = a.q + row * a.q_stride + (long long)((pl.head + g) * a.dim) * type_bytes(a.type);
+    const bool here = real && g < pl.n_q;
 #pragma unroll
     for (int j = 0; j < kChunk; ++j) q[g][j] = 0.f;
-    if (real && g < pl.n_q && pl.some) {
-      const char* p = a.q + row * a.q_stride + ((pl.head + g) * a.dim + pl.col) * type_bytes(a.type);
-      if (WIDE) read_chunk(a.type, p, q[g]);
-      else read_chunk(a.type, p, a.dim, q[g]);
+    if (!WIDE) {
+      if (here && pl.part == 0) read_chunk(a.type, p, a.dim, q[g]);
+      continue;
     }
 #pragma unroll
-    for (int j = 0; j < kChunk; ++j)
-      if (WIDE && pl.col + j < pl.part * kChunk) q[g][j] = 0.f;
+    for (int j = 0; j < kChunk / kPiece<TYPE>; ++j) {
+      bool some;
+      int skip;
+      const int col = first_column<TYPE, WIDE>(a, pl, j, &some, &skip);
+      if (here && some) {
+        if (TYPE == kE4M3) {
+          read_chunk(a.type, p + col * type_bytes(a.type), q[g]);
+        } else {
+          Chunk<TYPE> c;
+          c.w[0] = load_16(p + col * type_bytes(TYPE));
+#pragma unroll
+          for (int i = 0; i < kPiece<TYPE> / 2; ++i) c.pair(i, q[g][j * kPiece<TYPE> + 2 * i], q[g][j * kPiece<TYPE> + 2 * i + 1]);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < kPiece<TYPE>; ++i)
+        if (i < skip) q[g][j * kPiece<TYPE> + i] = 0.f;
+    }
+  }
+}
+
+// A lane's columns of a head of the output
+template <int TYPE, bool WIDE>
+__device__ __forceinline__ void write_out(const Attn& a, const Place& pl, char* p, const float (&y)[kChunk]) {
+  if (!WIDE) {
+    if (pl.part == 0) write_chunk(a.type, p, a.dim, false, y);
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j < kChunk / kPiece<TYPE>; ++j) {
+    bool some;
+    int skip;
+    const int col = first_column<TYPE, WIDE>(a, pl, j, &some, &skip);
+    if (!some) continue;
+    if (TYPE == kE4M3) {
+      write_chunk(a.type, p + col * type_bytes(a.type), kChunk, true, y);
+    } else if (TYPE == DCI_F32) {
+      store_16(p + col * 4, make_uint4(__float_as_uint(y[4 * j]), __float_as_uint(y[4 * j + 1]), __float_as_uint(y[4 * j + 2]), __float_as_uint(y[4 * j + 3])));
+    } else {
+      const int i = j * kPiece<TYPE>;
+      store_16(p + col * 2, make_uint4(two<TYPE>(y[i], y[i + 1]), two<TYPE>(y[i + 2], y[i + 3]), two<TYPE>(y[i + 4], y[i + 5]), two<TYPE>(y[i + 6], y[i + 7])));
+    }
   }
 }
 
@@ -323,7 +404,7 @@ __global__ __launch_bounds__(kAttnBlock, kWavesPerSimd<GQ>) void k_attn_chunks(c
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), p_lanes = 1 << a.p_log2;
   const unsigned unit = blockIdx.x * kAttnWaves + wave, c = unit / (unsigned)a.passes;  // wavefronts side by side read the same rows
   int heads_here, n_q;
-  const Place pl = place_of<GQ, WIDE>(a, (int)(unit - c * a.passes), 6 - a.p_log2, &heads_here, &n_q);
+  const Place pl = place_of<GQ>(a, (int)(unit - c * a.passes), 6 - a.p_log2, &heads_here, &n_q);
   const long long n = rows_of(a);
   if (c >= (unsigned)a.n_chunks || n == 0) return;
   const long long c0 = (long long)c * a.chunk, c1 = min(c0 + a.chunk, min(a.n_edges, a.indptr[n]));
@@ -333,12 +414,13 @@ __global__ __launch_bounds__(kAttnBlock, kWavesPerSimd<GQ>) void k_attn_chunks(c
     const long long row = piece ? last : first, b = a.indptr[row], e = a.indptr[row + 1];
     if (e - b <= a.chunk) continue;
     float q[GQ][kChunk];
-    read_q<GQ, WIDE>(a, pl, row, true, q);
+    const int source0 = first_source(a, pl, max(b, c0), min(e, c1), 6 - a.p_log2);
+    read_q<TYPE, GQ, WIDE>(a, pl, row, true, q);
     State<GQ> st;
     st.clear();
-    (void)attend<TYPE, GQ, BIAS, WIDE>(a, pl, max(b, c0), min(e, c1), 6 - a.p_log2, q, st, nullptr, a.scores);
+    (void)attend<TYPE, GQ, BIAS, WIDE>(a, pl, max(b, c0), min(e, c1), 6 - a.p_log2, source0, q, st, nullptr, a.scores);
     for (int apart = p_lanes; apart < kWave; apart <<= 1) join_lanes<GQ>(st, apart);
-    if (lane_id() < p_lanes && pl.some) {
+    if (lane_id() < p_lanes) {
 #pragma unroll
       for (int g = 0; g < GQ; ++g) {
         if (g < pl.n_q) {
@@ -347,7 +429,18 @@ __global__ __launch_bounds__(kAttnBlock, kWavesPerSimd<GQ>) void k_attn_chunks(c
             a.part_ml[2 * at] = st.m[g];
             a.part_ml[2 * at + 1] = st.l[g];
           }
-          write_chunk_as<DCI_F32>(reinterpret_cast<char*>(a.part_acc + at * ((a.dim + kChunk - 1) / kChunk * kChunk) + pl.col), kChunk, true, st.acc[g]);
+          float* acc = a.part_acc + at * ((a.dim + kChunk - 1) / kChunk * kChunk);
+#pragma unroll
+          for (int j = 0; j < kChunk / kPiece<TYPE>; ++j) {
+            bool some;
+            int skip;
+            const int col = first_column<TYPE, WIDE>(a, pl, j, &some, &skip);
+            if (!some) continue;
+#pragma unroll
+            for (int i = 0; i < (WIDE ? kPiece<TYPE> : kChunk); i += 4)
+              store_16(reinterpret_cast<char*>(acc + col + i), make_uint4(__float_as_uint(st.acc[g][j * kPiece<TYPE> + i]), __float_as_uint(st.acc[g][j * kPiece<TYPE> + i + 1]),
+                                                                          __float_as_uint(st.acc[g][j * kPiece<TYPE> + i + 2]), __float_as_uint(st.acc[g][j * kPiece<TYPE> + i + 3])));
+          }
         }
       }
     }
@@ -362,41 +455,60 @@ __global__ __launch_bounds__(kAttnBlock, kWavesPerSimd<GQ>) void k_attn_rows(con
   const int p_lanes = 1 << a.p_log2, groups = kWave >> a.p_log2, g_id = lane >> a.p_log2, r_log2 = a.r_log2;
   const unsigned unit = blockIdx.x * kAttnWaves + wave, turn = unit / (unsigned)a.passes;
   int heads_here, n_q;
-  const Place pl = place_of<GQ, WIDE>(a, (int)(unit - turn * a.passes), r_log2, &heads_here, &n_q);
+  const Place pl = place_of<GQ>(a, (int)(unit - turn * a.passes), r_log2, &heads_here, &n_q);
   const long long n = rows_of(a);
   const int at_once = groups >> r_log2;
   const unsigned turns = (unsigned)((n + at_once - 1) / at_once), step = gridDim.x * kAttnWaves / (unsigned)a.passes;
   float* stash = stash_all + wave * (kWave + groups) * a.stash_row;
+  // the bounds of the next rows are on their way while these are worked on, and so are, once these have been read, the next ones' sources
+  auto bounds = [&](unsigned k, long long* b, long long* e) {
+    const long long row = (long long)k * at_once + (g_id >> r_log2);
+    *b = *e = 0;
+    if (k < turns && row < n) {
+      *b = a.indptr[row];
+      *e = a.indptr[row + 1];
+    }
+  };
+  auto settle = [&](long long* b, long long* e) {  // false for a list that is cut
+    *b = max(0ll, *b);
+    *e = max(*b, min(a.n_edges, *e));
+    const bool here = !(a.n_chunks && *e - *b > a.chunk);
+    if (!here) *e = *b;
+    return here;
+  };
+  long long b, e;
+  bounds(turn, &b, &e);
+  bool here = settle(&b, &e);
+  int source0 = first_source(a, pl, b, e, r_log2);
   for (unsigned k = turn; k < turns; k += step) {
     const long long row = (long long)k * at_once + (g_id >> r_log2);
-    long long b = 0, e = 0;
-    if (row < n) {
-      b = a.indptr[row];
-      e = a.indptr[row + 1];
-    }
+    const bool mine = row < n && here;
+    long long next_b, next_e;
+    bounds(k + step >= k ? k + step : turns, &next_b, &next_e);
     float q[GQ][kChunk];
-    read_q<GQ, WIDE>(a, pl, row, row < n, q);
-    b = max(0ll, b);
-    e = max(b, min(a.n_edges, e));
-    const bool mine = row < n && !(a.n_chunks && e - b > a.chunk);
-    if (!mine) e = b;
+    read_q<TYPE, GQ, WIDE>(a, pl, row, mine, q);
     State<GQ> st;
     st.clear();
     // with weights: the scores of P << r_log2 entries at a time are gone through at the end, made anew if there are more
     const long long batch = p_lanes << r_log2;
     const bool whole = e - b <= batch;
-    const int named_all = attend<TYPE, GQ, BIAS, WIDE>(a, pl, b, e, r_log2, q, st, a.stash_row && whole ? stash : nullptr, nullptr);
+    const int named_all = attend<TYPE, GQ, BIAS, WIDE>(a, pl, b, e, r_log2, source0, q, st, a.stash_row && whole ? stash : nullptr, nullptr);
+    const long long first = b, last = e;
+    here = settle(&next_b, &next_e);
+    b = next_b;
+    e = next_e;
+    source0 = first_source(a, pl, b, e, r_log2);
     for (int apart = p_lanes; apart < p_lanes << r_log2; apart <<= 1) join_lanes<GQ>(st, apart);
     float lse[GQ];
 #pragma unroll
     for (int g = 0; g < GQ; ++g) {
       lse[g] = st.l[g] == 0.f ? -INFINITY : st.m[g] + log_of(st.l[g]);
-      if (mine && pl.sub == 0 && g < pl.n_q && pl.some) {
+      if (mine && pl.sub == 0 && g < pl.n_q) {
         const float inv = st.l[g] == 0.f ? 0.f : __builtin_amdgcn_rcpf(st.l[g]);
         float y[kChunk];
 #pragma unroll
         for (int j = 0; j < kChunk; ++j) y[j] = st.acc[g][j] * inv;
-        write_chunk(a.type, a.out + row * a.out_stride + ((pl.head + g) * a.dim + pl.col) * type_bytes(a.type), WIDE ? kChunk : a.dim, WIDE, y);
+        write_out<TYPE, WIDE>(a, pl, a.out + row * a.out_stride + (long long)((pl.head + g) * a.dim) * type_bytes(a.type), y);
         if (a.lse && pl.part == 0) a.lse[row * a.heads + pl.head + g] = lse[g];
       }
     }
@@ -407,12 +519,13 @@ __global__ __launch_bounds__(kAttnBlock, kWavesPerSimd<GQ>) void k_attn_rows(con
       for (int g = 0; g < GQ; ++g)
         if (g < pl.n_q) lses[pl.local + g] = lse[g];
     }
-    for (long long from = b; from < e; from += batch) {
+    for (long long from = first; from < last; from += batch) {
       int named_here = named_all;
       if (!whole) {
         State<GQ> unused;
         unused.clear();
-        named_here = attend<TYPE, GQ, BIAS, WIDE>(a, pl, from, min(e, from + batch), r_log2, q, unused, stash, nullptr);
+        const long long to = min(last, from + batch);
+        named_here = attend<TYPE, GQ, BIAS, WIDE>(a, pl, from, to, r_log2, first_source(a, pl, from, to, r_log2), q, unused, stash, nullptr);
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
@@ -541,17 +654,18 @@ __global__ __launch_bounds__(kAttnBlock) void k_attn_weights(const Attn a) {
 // How a call's work is cut, from its arguments alone (the workspace query has no context)
 struct Split {
   int p_log2, lh_log2, wave_heads, gq, gq_passes, passes;
-  bool wide;  // heads of 16 columns at least: read and written 16 at a time
+  bool wide;  // heads of 16 bytes at least: read and written 16 at a time
   int chunk;
   int64_t n_chunks;
 };
 constexpr int64_t kWantedWaves = 4096;  // 16 to a compute unit
 constexpr int kStashHeads = 32;  // query heads of a wavefront, at most, with weights: 40 KB of scores to a workgroup, four workgroups to a compute unit
 
-Split split_of(const dci_attn& t, bool accumulate) {
+// wide: see WIDE.  (The chunks, and so the workspace, do not depend on it.)
+Split split_of(const dci_attn& t, bool accumulate, bool wide) {
   Split s;
-  s.wide = t.head_dim >= kChunk;
-  const int group = t.n_heads / t.kv_heads, gq = group == 1 || !s.wide ? 1 : group == 2 ? 2 : 4;
+  s.wide = wide;
+  const int group = t.n_heads / t.kv_heads, gq = group == 1 ? 1 : group == 2 ? 2 : 4;
   s.lh_log2 = log2_up((t.head_dim + kChunk - 1) / kChunk);
   s.wave_heads = kWave >> s.lh_log2;
   if (accumulate && s.wave_heads > kStashHeads / gq) s.wave_heads = kStashHeads / gq;
@@ -559,12 +673,12 @@ Split split_of(const dci_attn& t, bool accumulate) {
   s.p_log2 = log2_up((int64_t)s.wave_heads << s.lh_log2);
   if (s.p_log2 < 2) s.p_log2 = 2;  // entries are taken four at a time
   const int parts = (t.kv_heads + s.wave_heads - 1) / s.wave_heads;
-  s.gq = gq;
+  s.gq = wide ? gq : 1;
   s.gq_passes = (group + s.gq - 1) / s.gq;
   s.passes = parts * s.gq_passes;
   // chunks of 64 to 512 entries: as long as there are wavefronts enough
   s.chunk = 64;
-  while (s.chunk < 512 && t.n_edges / s.chunk * s.passes > kWantedWaves) s.chunk *= 2;
+  while (s.chunk < 512 && t.n_edges / s.chunk * parts * ((group + gq - 1) / gq) > kWantedWaves) s.chunk *= 2;
   const int64_t longest = t.max_list > 0 && t.max_list < t.n_edges ? t.max_list : t.n_edges;
   s.n_chunks = longest > s.chunk ? (t.n_edges + s.chunk - 1) / s.chunk : 0;
   return s;
@@ -637,7 +751,7 @@ void launch_attn(const Split& s, const Attn& a, unsigned chunk_grid, unsigned ro
 }
 
 int32_t attn(dci_ctx* ctx, const dci_attn& t, int type, Attn a, bool accumulate) {
-  const Split s = split_of(t, accumulate);
+  const Split s = split_of(t, accumulate, t.head_dim * type_bytes(type) >= 16);
   Arena ar(ctx->ws, ctx->ws_bytes);
   const Parts parts = take_parts(ar, t, s, accumulate);
   if (!ar.ok()) {
@@ -689,7 +803,8 @@ int32_t attn(dci_ctx* ctx, const dci_attn& t, int type, Attn a, bool accumulate)
     ++a.r_log2;
   const int64_t at_once = 1ll << (groups_log2 - a.r_log2);
   int64_t blocks = ((t.n_rows + at_once - 1) / at_once * s.passes + kAttnWaves - 1) / kAttnWaves;
-  if (blocks > (int64_t)ctx->num_cus * 32) blocks = (int64_t)ctx->num_cus * 32;
+  const int64_t at_a_time = (int64_t)ctx->num_cus * (s.gq == 4 ? kWavesPerSimd<4> : s.gq == 2 ? kWavesPerSimd<2> : kWavesPerSimd<1>);
+  if (blocks > at_a_time) blocks = at_a_time;
   blocks = (blocks + s.passes - 1) / s.passes * s.passes;  // a wavefront keeps its share of the heads from row to row
   const unsigned chunk_grid = (unsigned)((s.n_chunks * s.passes + kAttnWaves - 1) / kAttnWaves), row_grid = (unsigned)blocks;
   const OnDevice on(ctx->device);
@@ -722,7 +837,7 @@ extern "C" {
 size_t dci_attn_workspace_bytes(const dci_attn* attn, int32_t accumulate) {
   if (!attn || !dci::sizes_ok(*attn) || attn->n_edges > dci::kMaxEdges) return 0;
   dci::Arena ar(nullptr, 0);
-  (void)dci::take_parts(ar, *attn, dci::split_of(*attn, accumulate != 0), accumulate != 0);
+  (void)dci::take_parts(ar, *attn, dci::split_of(*attn, accumulate != 0, true), accumulate != 0);
   return ar.off;
 }
 
