@@ -2,11 +2,11 @@
 //
 // For a row i and a head h, over the entries e of the row's list:  z_e = scale (q_i . K_e) + bias_e,  out = sum exp(z_e) V_e / sum exp(z_e).
 // One pass over the list: a running maximum m, the sum l of exp(z - m) and the accumulator of exp(z - m) V, the last two rescaled
-// when m grows.  Every K and V row that an entry names is read once, straight into registers, 16 columns to a lane:
-//   a head's columns lie in LH = 1 .. 16 adjacent lanes, in pieces of 16 bytes that follow each other from lane to lane (a lane has one of an 8-bit
-//   row, two of a 16-bit, four of a 32-bit one; the piece that a head ends in is its last 16 bytes, whichever of them the piece before has as well:
+// when m grows.  Every K and V row that an entry names is read once, straight into registers, 16 columns of an 8-bit row to a lane, 8 of others:
+//   a head's columns lie in LH = 1 .. 32 adjacent lanes, in pieces of 16 bytes that follow each other from lane to lane, so that a load asks for 128
+//   bytes in one place wherever a head has them (a lane has one piece, of a 32-bit row two; the piece that a head ends in is its last 16 bytes, whichever of them the piece before has as well:
 //   those count once in a score, and are written twice alike), the heads of a row side by side, P lanes in all (a power of two up to 64; more
-//   heads are shared out between wavefronts).  A score is a sum over LH lanes (DPP), and the lanes of a head then hold what they need
+//   heads are shared out between wavefronts).  A score is a sum over LH lanes, and the lanes of a head then hold what they need
 //   for their columns of the output: nothing passes through LDS.
 //   The 64 / P groups of lanes of a wavefront work on rows of their own, or R of them on one row, each on every R-th entry, and join their
 //   (m, l, acc) at the row's end.
@@ -30,6 +30,9 @@ constexpr float kLog2E = 1.44269504088896340736f;
 // wavefronts to a SIMD that the registers are shared out for
 template <int GQ>
 constexpr int kWavesPerSimd = GQ == 4 ? 2 : 3;
+// columns to a lane
+template <int TYPE>
+constexpr int kCols = TYPE == kE4M3 ? 16 : 8;
 constexpr double kWeightUnit = 4294967296.0;  // 2^32
 
 struct Attn {
@@ -78,16 +81,16 @@ struct Place {
   int local;  // the first one's number within the wavefront
 };
 
-template <int GQ>
+template <int GQ, int COLS>
 struct State {
-  float m[GQ], l[GQ], acc[GQ][kChunk];
+  float m[GQ], l[GQ], acc[GQ][COLS];
   __device__ __forceinline__ void clear() {
 #pragma unroll
     for (int g = 0; g < GQ; ++g) {
       m[g] = -INFINITY;
       l[g] = 0.f;
 #pragma unroll
-      for (int j = 0; j < kChunk; ++j) acc[g][j] = 0.f;
+      for (int j = 0; j < COLS; ++j) acc[g][j] = 0.f;
     }
   }
 };
@@ -122,6 +125,8 @@ __device__ __forceinline__ int named(const Attn& a, int s) {
 // heads are too narrow for a piece (!WIDE)
 template <int TYPE>
 constexpr int kPiece = 16 / type_bytes(TYPE);
+template <int TYPE>
+constexpr int kPieces = kCols<TYPE> / kPiece<TYPE>;
 template <int TYPE, bool WIDE>
 __device__ __forceinline__ int first_column(const Attn& a, const Place& pl, int j, bool* some, int* skip) {
   if (!WIDE) {
@@ -149,9 +154,9 @@ __device__ __forceinline__ int first_source(const Attn& a, const Place& pl, long
 // P << r_log2 named (there are no more where that is used).  stash (nullable): LDS for the scores, entry by entry of the wavefront; scores (nullable):
 // memory for them, entry by entry of the call.
 template <int TYPE, int GQ, bool BIAS, bool WIDE>
-__device__ __forceinline__ int attend(const Attn& a, const Place& pl, long long e0, long long e1, int r_log2, int source0, const float (&q)[GQ][kChunk],
-                                      State<GQ>& st, float* stash, float* scores) {
-  constexpr int U = TYPE == kE4M3 ? 4 : !WIDE ? 1 : TYPE == DCI_F32 ? 2 : 4;  // entries at a time
+__device__ __forceinline__ int attend(const Attn& a, const Place& pl, long long e0, long long e1, int r_log2, int source0, const float (&q)[GQ][kCols<TYPE>],
+                                      State<GQ, kCols<TYPE>>& st, float* stash, float* scores) {
+  constexpr int U = WIDE || TYPE == kE4M3 ? 4 : 1, C = kCols<TYPE>;  // entries at a time
   const int n = entries(a, e0, e1);
   const int* __restrict__ src = a.src + e0;
   const int lane = lane_id(), in = lane & ((1 << a.p_log2) - 1), base = lane - in;
@@ -161,14 +166,14 @@ __device__ __forceinline__ int attend(const Attn& a, const Place& pl, long long 
   if (n > 0) next = named(a, source0);
   const int width = TYPE == kE4M3 ? (a.dim + kChunk - 1) / kChunk * kChunk : a.dim;
   const char *k0 = a.k + (long long)(pl.kv * width) * type_bytes(TYPE), *v0 = a.v + (long long)(pl.kv * width) * type_bytes(TYPE);
-  int offset[Chunk<TYPE>::kWords];
+  int offset[Chunk<TYPE, C>::kWords];
 #pragma unroll
-  for (int j = 0; j < Chunk<TYPE>::kWords; ++j) {
+  for (int j = 0; j < Chunk<TYPE, C>::kWords; ++j) {
     bool some;
     int skip;
     offset[j] = first_column<TYPE, WIDE>(a, pl, j, &some, &skip) * type_bytes(TYPE);
   }
-  if (Chunk<TYPE>::kWords == 1) {
+  if (TYPE == kE4M3) {
     k0 += offset[0];
     v0 += offset[0];
   }
@@ -181,7 +186,7 @@ __device__ __forceinline__ int attend(const Attn& a, const Place& pl, long long 
     after = source(t0 + 2 * batch + first);
     const int mine = min(1 << a.p_log2, (n - t0 - pl.sub + (1 << r_log2) - 1) >> r_log2);  // entries of this group
     for (int u0 = 0; u0 < mine; u0 += U) {
-      Chunk<TYPE> kc[U], vc[U];
+      Chunk<TYPE, C> kc[U], vc[U];
       float ks[U], vs[U], bias[U][GQ];
       bool there[U];
 #pragma unroll
@@ -196,9 +201,9 @@ __device__ __forceinline__ int attend(const Attn& a, const Place& pl, long long 
           vc[u].load(pv);
         } else if (WIDE) {
 #pragma unroll
-          for (int j = 0; j < Chunk<TYPE>::kWords; ++j) kc[u].w[j] = load_16(pk + offset[j]);
+          for (int j = 0; j < Chunk<TYPE, C>::kWords; ++j) kc[u].w[j] = load_16(pk + offset[j]);
 #pragma unroll
-          for (int j = 0; j < Chunk<TYPE>::kWords; ++j) vc[u].w[j] = load_16(pv + offset[j]);
+          for (int j = 0; j < Chunk<TYPE, C>::kWords; ++j) vc[u].w[j] = load_16(pv + offset[j]);
         } else {
           kc[u].load(pk, a.dim, false);
           vc[u].load(pv, a.dim, false);
@@ -223,7 +228,7 @@ __device__ __forceinline__ int attend(const Attn& a, const Place& pl, long long 
 #pragma unroll
         for (int g = 0; g < GQ; ++g) z[u][g] = 0.f;
 #pragma unroll
-        for (int j = 0; j < kChunk / 2; ++j) {
+        for (int j = 0; j < C / 2; ++j) {
           float x, y;
           kc[u].pair(j, x, y);
 #pragma unroll
@@ -271,7 +276,7 @@ __device__ __forceinline__ int attend(const Attn& a, const Place& pl, long long 
           p[u][g] *= vs[u];
         }
 #pragma unroll
-        for (int j = 0; j < kChunk; ++j) st.acc[g][j] *= shrink;
+        for (int j = 0; j < C; ++j) st.acc[g][j] *= shrink;
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
@@ -280,7 +285,7 @@ __device__ __forceinline__ int attend(const Attn& a, const Place& pl, long long 
 #pragma unroll
         for (int g = 0; g < GQ; ++g) with[g] = !BIAS || z[u][g] != -INFINITY;
 #pragma unroll
-        for (int j = 0; j < kChunk / 2; ++j) {
+        for (int j = 0; j < C / 2; ++j) {
           float x, y;
           vc[u].pair(j, x, y);
 #pragma unroll
@@ -299,8 +304,8 @@ __device__ __forceinline__ int attend(const Attn& a, const Place& pl, long long 
 }
 
 // (m, l, acc) of lanes `apart` away joined into st
-template <int GQ>
-__device__ __forceinline__ void join_lanes(State<GQ>& st, int apart) {
+template <int GQ, int COLS>
+__device__ __forceinline__ void join_lanes(State<GQ, COLS>& st, int apart) {
 #pragma unroll
   for (int g = 0; g < GQ; ++g) {
     const float m2 = __shfl_xor(st.m[g], apart, kWave), l2 = __shfl_xor(st.l[g], apart, kWave);
@@ -309,7 +314,7 @@ __device__ __forceinline__ void join_lanes(State<GQ>& st, int apart) {
     st.m[g] = m;
     st.l[g] = st.l[g] * f1 + l2 * f2;
 #pragma unroll
-    for (int j = 0; j < kChunk; ++j) {
+    for (int j = 0; j < COLS; ++j) {
       const float other = __shfl_xor(st.acc[g][j], apart, kWave);
       st.acc[g][j] = st.acc[g][j] * f1 + other * f2;
     }
@@ -339,27 +344,27 @@ __device__ __forceinline__ Place place_of(const Attn& a, int pass, int r_log2, i
 }
 
 template <int TYPE, int GQ, bool WIDE>
-__device__ __forceinline__ void read_q(const Attn& a, const Place& pl, long long row, bool real, float (&q)[GQ][kChunk]) {
+__device__ __forceinline__ void read_q(const Attn& a, const Place& pl, long long row, bool real, float (&q)[GQ][kCols<TYPE>]) {
 #pragma unroll
   for (int g = 0; g < GQ; ++g) {
     const char* p = a.q + row * a.q_stride + (long long)((pl.head + g) * a.dim) * type_bytes(a.type);
     const bool here = real && g < pl.n_q;
 #pragma unroll
-    for (int j = 0; j < kChunk; ++j) q[g][j] = 0.f;
+    for (int j = 0; j < kCols<TYPE>; ++j) q[g][j] = 0.f;
     if (!WIDE) {
-      if (here && pl.part == 0) read_chunk(a.type, p, a.dim, q[g]);
+      if (here && pl.part == 0) read_chunk(a.type, p, a.dim, false, q[g]);
       continue;
     }
 #pragma unroll
-    for (int j = 0; j < kChunk / kPiece<TYPE>; ++j) {
+    for (int j = 0; j < kPieces<TYPE>; ++j) {
       bool some;
       int skip;
       const int col = first_column<TYPE, WIDE>(a, pl, j, &some, &skip);
       if (here && some) {
         if (TYPE == kE4M3) {
-          read_chunk(a.type, p + col * type_bytes(a.type), q[g]);
+          read_chunk(a.type, p + col * type_bytes(a.type), kChunk, true, q[g]);
         } else {
-          Chunk<TYPE> c;
+          Chunk<TYPE, kPiece<TYPE>> c;
           c.w[0] = load_16(p + col * type_bytes(TYPE));
 #pragma unroll
           for (int i = 0; i < kPiece<TYPE> / 2; ++i) c.pair(i, q[g][j * kPiece<TYPE> + 2 * i], q[g][j * kPiece<TYPE> + 2 * i + 1]);
@@ -374,13 +379,13 @@ __device__ __forceinline__ void read_q(const Attn& a, const Place& pl, long long
 
 // A lane's columns of a head of the output
 template <int TYPE, bool WIDE>
-__device__ __forceinline__ void write_out(const Attn& a, const Place& pl, char* p, const float (&y)[kChunk]) {
+__device__ __forceinline__ void write_out(const Attn& a, const Place& pl, char* p, const float (&y)[kCols<TYPE>]) {
   if (!WIDE) {
     if (pl.part == 0) write_chunk(a.type, p, a.dim, false, y);
     return;
   }
 #pragma unroll
-  for (int j = 0; j < kChunk / kPiece<TYPE>; ++j) {
+  for (int j = 0; j < kPieces<TYPE>; ++j) {
     bool some;
     int skip;
     const int col = first_column<TYPE, WIDE>(a, pl, j, &some, &skip);
@@ -413,13 +418,13 @@ __global__ __launch_bounds__(kAttnBlock, kWavesPerSimd<GQ>) void k_attn_chunks(c
   for (int piece = 0; piece < (first == last ? 1 : 2); ++piece) {
     const long long row = piece ? last : first, b = a.indptr[row], e = a.indptr[row + 1];
     if (e - b <= a.chunk) continue;
-    float q[GQ][kChunk];
+    float q[GQ][kCols<TYPE>];
     const int source0 = first_source(a, pl, max(b, c0), min(e, c1), 6 - a.p_log2);
     read_q<TYPE, GQ, WIDE>(a, pl, row, true, q);
-    State<GQ> st;
+    State<GQ, kCols<TYPE>> st;
     st.clear();
     (void)attend<TYPE, GQ, BIAS, WIDE>(a, pl, max(b, c0), min(e, c1), 6 - a.p_log2, source0, q, st, nullptr, a.scores);
-    for (int apart = p_lanes; apart < kWave; apart <<= 1) join_lanes<GQ>(st, apart);
+    for (int apart = p_lanes; apart < kWave; apart <<= 1) join_lanes(st, apart);
     if (lane_id() < p_lanes) {
 #pragma unroll
       for (int g = 0; g < GQ; ++g) {
@@ -431,13 +436,13 @@ __global__ __launch_bounds__(kAttnBlock, kWavesPerSimd<GQ>) void k_attn_chunks(c
           }
           float* acc = a.part_acc + at * ((a.dim + kChunk - 1) / kChunk * kChunk);
 #pragma unroll
-          for (int j = 0; j < kChunk / kPiece<TYPE>; ++j) {
+          for (int j = 0; j < kPieces<TYPE>; ++j) {
             bool some;
             int skip;
             const int col = first_column<TYPE, WIDE>(a, pl, j, &some, &skip);
             if (!some) continue;
 #pragma unroll
-            for (int i = 0; i < (WIDE ? kPiece<TYPE> : kChunk); i += 4)
+            for (int i = 0; i < (WIDE ? kPiece<TYPE> : kCols<TYPE>); i += 4)
               store_16(reinterpret_cast<char*>(acc + col + i), make_uint4(__float_as_uint(st.acc[g][j * kPiece<TYPE> + i]), __float_as_uint(st.acc[g][j * kPiece<TYPE> + i + 1]),
                                                                           __float_as_uint(st.acc[g][j * kPiece<TYPE> + i + 2]), __float_as_uint(st.acc[g][j * kPiece<TYPE> + i + 3])));
           }
@@ -485,9 +490,9 @@ __global__ __launch_bounds__(kAttnBlock, kWavesPerSimd<GQ>) void k_attn_rows(con
     const bool mine = row < n && here;
     long long next_b, next_e;
     bounds(k + step >= k ? k + step : turns, &next_b, &next_e);
-    float q[GQ][kChunk];
+    float q[GQ][kCols<TYPE>];
     read_q<TYPE, GQ, WIDE>(a, pl, row, mine, q);
-    State<GQ> st;
+    State<GQ, kCols<TYPE>> st;
     st.clear();
     // with weights: the scores of P << r_log2 entries at a time are gone through at the end, made anew if there are more
     const long long batch = p_lanes << r_log2;
@@ -498,16 +503,16 @@ __global__ __launch_bounds__(kAttnBlock, kWavesPerSimd<GQ>) void k_attn_rows(con
     b = next_b;
     e = next_e;
     source0 = first_source(a, pl, b, e, r_log2);
-    for (int apart = p_lanes; apart < p_lanes << r_log2; apart <<= 1) join_lanes<GQ>(st, apart);
+    for (int apart = p_lanes; apart < p_lanes << r_log2; apart <<= 1) join_lanes(st, apart);
     float lse[GQ];
 #pragma unroll
     for (int g = 0; g < GQ; ++g) {
       lse[g] = st.l[g] == 0.f ? -INFINITY : st.m[g] + log_of(st.l[g]);
       if (mine && pl.sub == 0 && g < pl.n_q) {
         const float inv = st.l[g] == 0.f ? 0.f : __builtin_amdgcn_rcpf(st.l[g]);
-        float y[kChunk];
+        float y[kCols<TYPE>];
 #pragma unroll
-        for (int j = 0; j < kChunk; ++j) y[j] = st.acc[g][j] * inv;
+        for (int j = 0; j < kCols<TYPE>; ++j) y[j] = st.acc[g][j] * inv;
         write_out<TYPE, WIDE>(a, pl, a.out + row * a.out_stride + (long long)((pl.head + g) * a.dim) * type_bytes(a.type), y);
         if (a.lse && pl.part == 0) a.lse[row * a.heads + pl.head + g] = lse[g];
       }
@@ -522,7 +527,7 @@ __global__ __launch_bounds__(kAttnBlock, kWavesPerSimd<GQ>) void k_attn_rows(con
     for (long long from = first; from < last; from += batch) {
       int named_here = named_all;
       if (!whole) {
-        State<GQ> unused;
+        State<GQ, kCols<TYPE>> unused;
         unused.clear();
         const long long to = min(last, from + batch);
         named_here = attend<TYPE, GQ, BIAS, WIDE>(a, pl, from, to, r_log2, first_source(a, pl, from, to, r_log2), q, unused, stash, nullptr);
@@ -661,24 +666,24 @@ struct Split {
 constexpr int64_t kWantedWaves = 4096;  // 16 to a compute unit
 constexpr int kStashHeads = 32;  // query heads of a wavefront, at most, with weights: 40 KB of scores to a workgroup, four workgroups to a compute unit
 
-// wide: see WIDE.  (The chunks, and so the workspace, do not depend on it.)
-Split split_of(const dci_attn& t, bool accumulate, bool wide) {
+// cols: columns to a lane; wide: heads are not narrower than a piece.  (The chunks, and so the workspace, do not depend on them.)
+Split split_of(const dci_attn& t, bool accumulate, int cols, bool wide) {
   Split s;
   s.wide = wide;
   const int group = t.n_heads / t.kv_heads, gq = group == 1 ? 1 : group == 2 ? 2 : 4;
-  s.lh_log2 = log2_up((t.head_dim + kChunk - 1) / kChunk);
+  s.gq = wide ? gq : 1;
+  s.gq_passes = (group + s.gq - 1) / s.gq;
+  s.lh_log2 = log2_up((t.head_dim + cols - 1) / cols);
   s.wave_heads = kWave >> s.lh_log2;
   if (accumulate && s.wave_heads > kStashHeads / gq) s.wave_heads = kStashHeads / gq;
   if (s.wave_heads > t.kv_heads) s.wave_heads = t.kv_heads;
   s.p_log2 = log2_up((int64_t)s.wave_heads << s.lh_log2);
   if (s.p_log2 < 2) s.p_log2 = 2;  // entries are taken four at a time
-  const int parts = (t.kv_heads + s.wave_heads - 1) / s.wave_heads;
-  s.gq = wide ? gq : 1;
-  s.gq_passes = (group + s.gq - 1) / s.gq;
-  s.passes = parts * s.gq_passes;
-  // chunks of 64 to 512 entries: as long as there are wavefronts enough
+  s.passes = (t.kv_heads + s.wave_heads - 1) / s.wave_heads * s.gq_passes;
+  // chunks of 64 to 512 entries: as long as there are wavefronts enough, 64 lanes of 16 columns each
+  const int64_t waves = ((int64_t)t.kv_heads * kv_width(t.head_dim) + 1023) / 1024 * ((group + gq - 1) / gq);
   s.chunk = 64;
-  while (s.chunk < 512 && t.n_edges / s.chunk * parts * ((group + gq - 1) / gq) > kWantedWaves) s.chunk *= 2;
+  while (s.chunk < 512 && t.n_edges / s.chunk * waves > kWantedWaves) s.chunk *= 2;
   const int64_t longest = t.max_list > 0 && t.max_list < t.n_edges ? t.max_list : t.n_edges;
   s.n_chunks = longest > s.chunk ? (t.n_edges + s.chunk - 1) / s.chunk : 0;
   return s;
@@ -751,7 +756,7 @@ void launch_attn(const Split& s, const Attn& a, unsigned chunk_grid, unsigned ro
 }
 
 int32_t attn(dci_ctx* ctx, const dci_attn& t, int type, Attn a, bool accumulate) {
-  const Split s = split_of(t, accumulate, t.head_dim * type_bytes(type) >= 16);
+  const Split s = split_of(t, accumulate, type == kE4M3 ? kCols<kE4M3> : kCols<DCI_F32>, t.head_dim * type_bytes(type) >= 16);
   Arena ar(ctx->ws, ctx->ws_bytes);
   const Parts parts = take_parts(ar, t, s, accumulate);
   if (!ar.ok()) {
@@ -837,7 +842,7 @@ extern "C" {
 size_t dci_attn_workspace_bytes(const dci_attn* attn, int32_t accumulate) {
   if (!attn || !dci::sizes_ok(*attn) || attn->n_edges > dci::kMaxEdges) return 0;
   dci::Arena ar(nullptr, 0);
-  (void)dci::take_parts(ar, *attn, dci::split_of(*attn, accumulate != 0, true), accumulate != 0);
+  (void)dci::take_parts(ar, *attn, dci::split_of(*attn, accumulate != 0, dci::kChunk, true), accumulate != 0);
   return ar.off;
 }
 

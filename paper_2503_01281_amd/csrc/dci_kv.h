@@ -54,10 +54,10 @@ __device__ __forceinline__ void store_16(char* p, uint4 v) {
   *reinterpret_cast<u32x4_any*>(p) = u;
 }
 
-// 16 columns of a row as they lie in memory.
-template <int TYPE>
+// COLS columns of a row as they lie in memory.
+template <int TYPE, int COLS = kChunk>
 struct Chunk {
-  static constexpr int kWords = type_bytes(TYPE);  // of 16 bytes
+  static constexpr int kWords = type_bytes(TYPE) * COLS / 16;  // of 16 bytes
   uint4 w[kWords];
 
   __device__ __forceinline__ void clear() {
@@ -68,20 +68,20 @@ struct Chunk {
 #pragma unroll
     for (int j = 0; j < kWords; ++j) w[j] = load_16(p + 16 * j);
   }
-  // The first `cols` (1 .. 16) of them from p, the others 0; wide: by 16 bytes (by_16_bytes), else number by number.
+  // The first `cols` (1 .. COLS) of them from p, the others 0; wide: by 16 bytes (by_16_bytes), else number by number.
   __device__ __forceinline__ void load(const char* p, int cols, bool wide) {
     if (TYPE == kE4M3) {
       w[0] = *reinterpret_cast<const uint4*>(p);
     } else if (wide) {
 #pragma unroll
       for (int j = 0; j < kWords; ++j)
-        w[j] = j * (16 / type_bytes(TYPE)) < cols ? reinterpret_cast<const uint4*>(p)[j] : make_uint4(0, 0, 0, 0);
+        w[j] = j * (16 / type_bytes(TYPE)) < cols ? load_16(p + 16 * j) : make_uint4(0, 0, 0, 0);
     } else {
       unsigned u[kWords * 4];
 #pragma unroll
       for (int j = 0; j < kWords * 4; ++j) u[j] = 0;
 #pragma unroll
-      for (int j = 0; j < kChunk; ++j) {
+      for (int j = 0; j < COLS; ++j) {
         if (j < cols) {
           if (TYPE == DCI_F32) u[j] = reinterpret_cast<const unsigned*>(p)[j];
           else u[j / 2] |= (unsigned)reinterpret_cast<const unsigned short*>(p)[j] << (16 * (j & 1));
@@ -118,37 +118,19 @@ struct Chunk {
 };
 
 // 16 columns from p as numbers
-template <int TYPE>
-__device__ __forceinline__ void read_chunk_as(const char* p, int cols, bool wide, float (&x)[kChunk]) {
-  Chunk<TYPE> c;
+template <int TYPE, int COLS>
+__device__ __forceinline__ void read_chunk_as(const char* p, int cols, bool wide, float (&x)[COLS]) {
+  Chunk<TYPE, COLS> c;
   c.load(p, cols, wide);
 #pragma unroll
-  for (int j = 0; j < kChunk / 2; ++j) c.pair(j, x[2 * j], x[2 * j + 1]);
+  for (int j = 0; j < COLS / 2; ++j) c.pair(j, x[2 * j], x[2 * j + 1]);
 }
-// Whatever their type, all 16 or the first `cols`
-__device__ __forceinline__ void read_chunk(int type, const char* p, float (&x)[kChunk]) {
-  Chunk<DCI_F32> c;
-  if (type == DCI_F32) {
-    c.load(p);
-#pragma unroll
-    for (int j = 0; j < kChunk / 2; ++j) c.pair(j, x[2 * j], x[2 * j + 1]);
-  } else {
-    Chunk<DCI_BF16> b;
-    Chunk<DCI_F16> h;
-    b.load(p);
-#pragma unroll
-    for (int j = 0; j < 2; ++j) h.w[j] = b.w[j];
-#pragma unroll
-    for (int j = 0; j < kChunk / 2; ++j) {
-      if (type == DCI_BF16) b.pair(j, x[2 * j], x[2 * j + 1]);
-      else h.pair(j, x[2 * j], x[2 * j + 1]);
-    }
-  }
-}
-__device__ __forceinline__ void read_chunk(int type, const char* p, int cols, float (&x)[kChunk]) {
-  if (type == DCI_F32) read_chunk_as<DCI_F32>(p, cols, false, x);
-  else if (type == DCI_BF16) read_chunk_as<DCI_BF16>(p, cols, false, x);
-  else read_chunk_as<DCI_F16>(p, cols, false, x);
+// Whatever their type
+template <int COLS>
+__device__ __forceinline__ void read_chunk(int type, const char* p, int cols, bool wide, float (&x)[COLS]) {
+  if (type == DCI_F32) read_chunk_as<DCI_F32>(p, cols, wide, x);
+  else if (type == DCI_BF16) read_chunk_as<DCI_BF16>(p, cols, wide, x);
+  else read_chunk_as<DCI_F16>(p, cols, wide, x);
 }
 
 template <int TYPE>
@@ -163,22 +145,22 @@ __device__ __forceinline__ unsigned two(float a, float b) {  // both rounded to 
   const h2 h = {(_Float16)a, (_Float16)b};
   return __builtin_bit_cast(unsigned, h);
 }
-template <int TYPE>
-__device__ __forceinline__ void write_chunk_as(char* p, int cols, bool wide, const float (&x)[kChunk]) {
+template <int TYPE, int COLS>
+__device__ __forceinline__ void write_chunk_as(char* p, int cols, bool wide, const float (&x)[COLS]) {
   constexpr int kPer = 16 / type_bytes(TYPE);
-  unsigned u[kChunk * type_bytes(TYPE) / 4];
+  unsigned u[COLS * type_bytes(TYPE) / 4];
 #pragma unroll
-  for (int j = 0; j < kChunk; ++j) {
+  for (int j = 0; j < COLS; ++j) {
     if (TYPE == DCI_F32) u[j] = __float_as_uint(x[j]);
     else if (j % 2 == 0) u[j / 2] = two<TYPE>(x[j], x[j + 1]);
   }
   if (wide) {
 #pragma unroll
-    for (int j = 0; j < type_bytes(TYPE); ++j)
+    for (int j = 0; j < COLS / kPer; ++j)
       if (j * kPer < cols) store_16(p + 16 * j, make_uint4(u[4 * j], u[4 * j + 1], u[4 * j + 2], u[4 * j + 3]));
   } else {
 #pragma unroll
-    for (int j = 0; j < kChunk; ++j) {
+    for (int j = 0; j < COLS; ++j) {
       if (j < cols) {
         if (TYPE == DCI_F32) reinterpret_cast<unsigned*>(p)[j] = u[j];
         else reinterpret_cast<unsigned short*>(p)[j] = (unsigned short)(u[j / 2] >> (16 * (j & 1)));
@@ -186,7 +168,8 @@ __device__ __forceinline__ void write_chunk_as(char* p, int cols, bool wide, con
     }
   }
 }
-__device__ __forceinline__ void write_chunk(int type, char* p, int cols, bool wide, const float (&x)[kChunk]) {
+template <int COLS>
+__device__ __forceinline__ void write_chunk(int type, char* p, int cols, bool wide, const float (&x)[COLS]) {
   if (type == DCI_F32) write_chunk_as<DCI_F32>(p, cols, wide, x);
   else if (type == DCI_BF16) write_chunk_as<DCI_BF16>(p, cols, wide, x);
   else write_chunk_as<DCI_F16>(p, cols, wide, x);
@@ -197,7 +180,7 @@ template <int CTRL>
 __device__ __forceinline__ float dpp(float x) {
   return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xF, 0xF, true));
 }
-// Sums of N numbers each over groups of 1 << log2 lanes (log2 <= 4), in all of the lanes
+// Sums of N numbers each over groups of 1 << log2 lanes (log2 <= 5), in all of the lanes
 template <int N>
 __device__ __forceinline__ void sum_lanes(float* x, int log2) {
 #define DCI_STEP(STEP_, CTRL_)                              \
@@ -209,6 +192,10 @@ __device__ __forceinline__ void sum_lanes(float* x, int log2) {
   DCI_STEP(2, 0x141)  // the other half of eight, mirrored
   DCI_STEP(3, 0x140)  // the other half of sixteen, mirrored
 #undef DCI_STEP
+  if (log2 > 4) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] += __shfl_xor(x[i], 16, kWave);
+  }
 }
 // The maximum likewise
 __device__ __forceinline__ float max_lanes(float x, int log2) {
