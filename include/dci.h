@@ -501,7 +501,8 @@ typedef struct {
   const int32_t* src;      /* device [n_edges]                                                         */
   int64_t n_edges;         /* entries in src (a bound on indptr's last value)                          */
   int64_t n_src;           /* sources: rows of dense k and v, entries of slots; 0 .. 2^31-1            */
-  int32_t max_list;        /* no list is longer, as by a fan-out; 0: not known.  Only the work split depends on it */
+  int32_t max_list;        /* entries of a list that count, from its first on, as by a fan-out (0: all of them).  A call that
+                              says so, where lists have at most 64, need not look for longer ones            */
   int32_t dtype;           /* DCI_F32, DCI_BF16 or DCI_F16: of q, out and dense k, v                   */
   int32_t n_heads;         /* a multiple of kv_heads, at most DCI_MAX_HEADS                            */
   int32_t kv_heads;
@@ -517,7 +518,7 @@ typedef struct {
 } dci_attn;
 
 /* Workspace of an attention call (accumulate as for dci_attn_cached): lists longer than 64 to 512 entries (the more entries there are in all, the
- * longer) are cut, and their parts joined from there; with accumulate their scores are kept there.  0 where max_list says that there are no such
+ * longer) are cut, and their parts joined from there; with accumulate those longer than 64 are, and their scores are kept there.  0 where max_list says that there are no such
  * lists.  It depends on n_rows, n_edges, max_list, heads, head_dim and accumulate only. */
 size_t dci_attn_workspace_bytes(const dci_attn* attn, int32_t accumulate);
 

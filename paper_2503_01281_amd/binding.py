@@ -572,8 +572,8 @@ def dci_attn_forward(ctx: Context, q: torch.Tensor, k: torch.Tensor, v: torch.Te
                      n_dev: Optional[int] = None, max_list: int = 0):
     """Rows attend over their lists of dense rows: ``q``, ``out`` [n, n_heads, head_dim], ``k``, ``v`` [n_src, kv_heads, head_dim], of one
     type (fp32, bf16 or fp16), rows strided as they like; ``indptr`` int64 [n + 1], ``src`` int32 [n_edges]; ``lse`` fp32 [n, n_heads];
-    ``bias`` fp32 [n_edges, 1 or n_heads].  ``n_dev``: device address of an int64 row count, n is then its bound; ``max_list``: no list
-    is longer (0: not known)."""
+    ``bias`` fp32 [n_edges, 1 or n_heads].  ``n_dev``: device address of an int64 row count, n is then its bound; ``max_list``: how many
+    entries of a list count (0: all of them)."""
     assert k.dtype == q.dtype and v.dtype == q.dtype and k.shape == v.shape
     a = _attn_args(q, k.shape[1], k.shape[0], indptr, src, out, scale, lse, bias, n_dev, max_list)
     need = ctx.lib.dci_attn_workspace_bytes(C.byref(a), 0)

@@ -27,9 +27,8 @@ namespace {
 
 constexpr int kAttnBlock = 256, kAttnWaves = kAttnBlock / kWave;
 constexpr float kLog2E = 1.44269504088896340736f;
-// wavefronts to a SIMD that the registers are shared out for
-template <int GQ>
-constexpr int kWavesPerSimd = GQ == 4 ? 2 : 3;
+// wavefronts to a SIMD that the registers are shared out for: as many as there are without spilling
+constexpr int waves_per_simd(int type, int gq) { return gq == 4 ? 2 : gq == 2 ? 3 : type == DCI_F32 || type == kE4M3 ? 3 : 4; }
 // columns to a lane
 template <int TYPE>
 constexpr int kCols = TYPE == kE4M3 ? 16 : 8;
@@ -64,6 +63,7 @@ struct Attn {
   int gq_passes;                // of them, those that share a group
   int chunk;
   int n_chunks;  // 0: no list is cut
+  long long longest;  // entries of a list that count
   int stash_row;  // with weights: floats of LDS for the scores of an entry (an odd number, against bank conflicts), 0 without
   float* part_ml;   // [2 n_chunks, heads, 2]
   float* part_acc;  // [2 n_chunks, heads, W]
@@ -405,7 +405,7 @@ __device__ __forceinline__ long long rows_of(const Attn& a) { return a.n_dev ? m
 
 // A chunk to a wavefront: the pieces of up to two long lists, left in the workspace
 template <int TYPE, int GQ, bool BIAS, bool WIDE>
-__global__ __launch_bounds__(kAttnBlock, kWavesPerSimd<GQ>) void k_attn_chunks(const Attn a) {
+__global__ __launch_bounds__(kAttnBlock, waves_per_simd(TYPE, GQ)) void k_attn_chunks(const Attn a) {
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), p_lanes = 1 << a.p_log2;
   const unsigned unit = blockIdx.x * kAttnWaves + wave, c = unit / (unsigned)a.passes;  // wavefronts side by side read the same rows
   int heads_here, n_q;
@@ -416,8 +416,8 @@ __global__ __launch_bounds__(kAttnBlock, kWavesPerSimd<GQ>) void k_attn_chunks(c
   if (c0 >= c1) return;
   const long long first = row_of(a.indptr, n, c0), last = row_of(a.indptr, n, c1 - 1);
   for (int piece = 0; piece < (first == last ? 1 : 2); ++piece) {
-    const long long row = piece ? last : first, b = a.indptr[row], e = a.indptr[row + 1];
-    if (e - b <= a.chunk) continue;
+    const long long row = piece ? last : first, b = a.indptr[row], e = min(a.indptr[row + 1], b + a.longest);
+    if (e - b <= a.chunk || c0 >= e) continue;
     float q[GQ][kCols<TYPE>];
     const int source0 = first_source(a, pl, max(b, c0), min(e, c1), 6 - a.p_log2);
     read_q<TYPE, GQ, WIDE>(a, pl, row, true, q);
@@ -454,7 +454,7 @@ __global__ __launch_bounds__(kAttnBlock, kWavesPerSimd<GQ>) void k_attn_chunks(c
 
 // Rows, one or more to a wavefront, one set after the other; cut lists are not its business
 template <int TYPE, int GQ, bool BIAS, bool WIDE>
-__global__ __launch_bounds__(kAttnBlock, kWavesPerSimd<GQ>) void k_attn_rows(const Attn a) {
+__global__ __launch_bounds__(kAttnBlock, waves_per_simd(TYPE, GQ)) void k_attn_rows(const Attn a) {
   extern __shared__ float stash_all[];
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
   const int p_lanes = 1 << a.p_log2, groups = kWave >> a.p_log2, g_id = lane >> a.p_log2, r_log2 = a.r_log2;
@@ -476,7 +476,7 @@ __global__ __launch_bounds__(kAttnBlock, kWavesPerSimd<GQ>) void k_attn_rows(con
   };
   auto settle = [&](long long* b, long long* e) {  // false for a list that is cut
     *b = max(0ll, *b);
-    *e = max(*b, min(a.n_edges, *e));
+    *e = max(*b, min(min(a.n_edges, *e), *b + a.longest));
     const bool here = !(a.n_chunks && *e - *b > a.chunk);
     if (!here) *e = *b;
     return here;
@@ -494,11 +494,7 @@ __global__ __launch_bounds__(kAttnBlock, kWavesPerSimd<GQ>) void k_attn_rows(con
     read_q<TYPE, GQ, WIDE>(a, pl, row, mine, q);
     State<GQ, kCols<TYPE>> st;
     st.clear();
-    // with weights: the scores of P << r_log2 entries at a time are gone through at the end, made anew if there are more
-    const long long batch = p_lanes << r_log2;
-    const bool whole = e - b <= batch;
-    const int named_all = attend<TYPE, GQ, BIAS, WIDE>(a, pl, b, e, r_log2, source0, q, st, a.stash_row && whole ? stash : nullptr, nullptr);
-    const long long first = b, last = e;
+    const int names = attend<TYPE, GQ, BIAS, WIDE>(a, pl, b, e, r_log2, source0, q, st, a.stash_row ? stash : nullptr, nullptr);
     here = settle(&next_b, &next_e);
     b = next_b;
     e = next_e;
@@ -524,33 +520,24 @@ __global__ __launch_bounds__(kAttnBlock, kWavesPerSimd<GQ>) void k_attn_rows(con
       for (int g = 0; g < GQ; ++g)
         if (g < pl.n_q) lses[pl.local + g] = lse[g];
     }
-    for (long long from = first; from < last; from += batch) {
-      int named_here = named_all;
-      if (!whole) {
-        State<GQ, kCols<TYPE>> unused;
-        unused.clear();
-        const long long to = min(last, from + batch);
-        named_here = attend<TYPE, GQ, BIAS, WIDE>(a, pl, from, to, r_log2, first_source(a, pl, from, to, r_log2), q, unused, stash, nullptr);
-      }
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      __builtin_amdgcn_wave_barrier();
-      if (named_here >= 0) {  // every lane its own entry, over the wavefront's heads
-        const float* zs = stash + lane * a.stash_row;
-        float p = 0.f;
-        for (int h = 0; h < heads_here; ++h) {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    if (names >= 0) {  // every lane its own entry, over the wavefront's heads
+      const float* zs = stash + lane * a.stash_row;
+      float p = 0.f;
+      for (int h = 0; h < heads_here; ++h) {
 #pragma unroll
-          for (int g = 0; g < GQ; ++g) {
-            if (g < n_q) {
-              const float z = zs[h * GQ + g];
-              if (z != -INFINITY) p += exp_diff(z, lses[h * GQ + g]);
-            }
+        for (int g = 0; g < GQ; ++g) {
+          if (g < n_q) {
+            const float z = zs[h * GQ + g];
+            if (z != -INFINITY) p += exp_diff(z, lses[h * GQ + g]);
           }
         }
-        add_weight(a, named_here, p);
       }
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      __builtin_amdgcn_wave_barrier();
+      add_weight(a, names, p);
     }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
   }
 }
 
@@ -570,7 +557,7 @@ __global__ __launch_bounds__(kAttnBlock) void k_attn_join(const Attn a, bool by_
     row = row_of(a.indptr, n, c1 - 1);
     if (a.indptr[row] < c0) return;
   }
-  const long long b = a.indptr[row], e = min(a.n_edges, a.indptr[row + 1]);
+  const long long b = a.indptr[row], e = min(min(a.n_edges, a.indptr[row + 1]), b + a.longest);
   if (b < 0 || e - b <= a.chunk) return;
   const long long c = b / a.chunk;
   const int width = (a.dim + kChunk - 1) / kChunk * kChunk;
@@ -641,7 +628,7 @@ __global__ __launch_bounds__(kAttnBlock) void k_attn_weights(const Attn a) {
   for (int piece = 0; piece < 2; ++piece) {
     const long long row = piece ? last : first;
     if (piece && first == last) break;
-    const long long b = a.indptr[row], e = a.indptr[row + 1];
+    const long long b = a.indptr[row], e = min(a.indptr[row + 1], b + a.longest);
     if (e - b <= a.chunk) continue;
     const long long to = min(e, c1);
     for (long long t = max(b, c0) + lane_id(); t < to; t += kWave) {
@@ -680,10 +667,11 @@ Split split_of(const dci_attn& t, bool accumulate, int cols, bool wide) {
   s.p_log2 = log2_up((int64_t)s.wave_heads << s.lh_log2);
   if (s.p_log2 < 2) s.p_log2 = 2;  // entries are taken four at a time
   s.passes = (t.kv_heads + s.wave_heads - 1) / s.wave_heads * s.gq_passes;
-  // chunks of 64 to 512 entries: as long as there are wavefronts enough, 64 lanes of 16 columns each
+  // chunks of 64 to 512 entries: as long as there are wavefronts enough, 64 lanes of 16 columns each; of 64 with weights, as a wavefront then keeps
+  // the scores of the lists that are not cut
   const int64_t waves = ((int64_t)t.kv_heads * kv_width(t.head_dim) + 1023) / 1024 * ((group + gq - 1) / gq);
   s.chunk = 64;
-  while (s.chunk < 512 && t.n_edges / s.chunk * waves > kWantedWaves) s.chunk *= 2;
+  while (!accumulate && s.chunk < 512 && t.n_edges / s.chunk * waves > kWantedWaves) s.chunk *= 2;
   const int64_t longest = t.max_list > 0 && t.max_list < t.n_edges ? t.max_list : t.n_edges;
   s.n_chunks = longest > s.chunk ? (t.n_edges + s.chunk - 1) / s.chunk : 0;
   return s;
@@ -798,6 +786,7 @@ int32_t attn(dci_ctx* ctx, const dci_attn& t, int type, Attn a, bool accumulate)
   a.gq_passes = s.gq_passes;
   a.chunk = s.chunk;
   a.n_chunks = (int)s.n_chunks;
+  a.longest = t.max_list > 0 ? t.max_list : t.n_edges;
   // lane groups to a row: one, unless that leaves wavefronts to be had (no more then than there are entries in a list) or, with weights, the scores
   // of the longest list would not all be at hand at its end
   const int groups_log2 = 6 - s.p_log2;
@@ -808,7 +797,7 @@ int32_t attn(dci_ctx* ctx, const dci_attn& t, int type, Attn a, bool accumulate)
     ++a.r_log2;
   const int64_t at_once = 1ll << (groups_log2 - a.r_log2);
   int64_t blocks = ((t.n_rows + at_once - 1) / at_once * s.passes + kAttnWaves - 1) / kAttnWaves;
-  const int64_t at_a_time = (int64_t)ctx->num_cus * (s.gq == 4 ? kWavesPerSimd<4> : s.gq == 2 ? kWavesPerSimd<2> : kWavesPerSimd<1>);
+  const int64_t at_a_time = (int64_t)ctx->num_cus * waves_per_simd(type, s.gq);
   if (blocks > at_a_time) blocks = at_a_time;
   blocks = (blocks + s.passes - 1) / s.passes * s.passes;  // a wavefront keeps its share of the heads from row to row
   const unsigned chunk_grid = (unsigned)((s.n_chunks * s.passes + kAttnWaves - 1) / kAttnWaves), row_grid = (unsigned)blocks;

@@ -67,6 +67,10 @@ def cached_case(dci, ctx, lengths, heads, kv, dim, dtype, seed, block=16, n_slot
         inside = (where >= 0) & (where < sources)
         where = np.where(inside, slots[np.where(inside, where, 0)], -1)
         where = np.where((where >= 0) & (where < n_slots), where, -1)
+    if max_list:
+        where = where.copy()
+        for i in range(n):
+            where[indptr[i] + max_list:indptr[i + 1]] = -1
     q = rounded(rng.standard_normal((n, heads, dim)).astype(np.float32), dtype)
     bias = None
     if bias_heads:
@@ -134,12 +138,12 @@ def test_cached_few_rows(lengths, accumulate):
     cached_case(dci, dci.Context(0), lengths, 4, 4, 64, "fp32", seed=len(lengths), accumulate=accumulate)
 
 
-def test_what_max_list_says_does_not_matter():
-    """Too small a bound, the right one or none: lists are attended to whole."""
+@pytest.mark.parametrize("max_list", [1, 5, 16, 64, 65, 100, 128, 320, 699, 700, 10 ** 6])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_entries_beyond_max_list_do_not_count(max_list, accumulate):
+    """Lists of up to 700 entries, of which the first max_list count."""
     import paper_2503_01281_amd as dci
-    ctx = dci.Context(0)
-    for max_list in (0, 1, 64, 700, 10 ** 6):
-        cached_case(dci, ctx, CUT, 4, 4, 32, "bf16", seed=3, max_list=max_list)
+    cached_case(dci, dci.Context(0), CUT, 4, 4, 32, "bf16", seed=3, max_list=max_list, accumulate=accumulate)
 
 
 @pytest.mark.parametrize("heads,kv,dim,dtype", [(4, 4, 64, "fp32"), (4, 4, 64, "bf16"), (8, 2, 128, "fp16"), (3, 3, 41, "fp16"), (3, 1, 41, "bf16"),
