@@ -61,6 +61,7 @@ struct Attn {
   int wave_heads;               // key heads to a wavefront
   int passes;                   // wavefronts that share a row's key heads and their groups
   int gq_passes;                // of them, those that share a group
+  int pass_heads;               // query heads to one of those, in k_attn_groups
   int chunk;
   int n_chunks;  // 0: no list is cut
   long long longest;  // entries of a list that count
@@ -541,6 +542,259 @@ __global__ __launch_bounds__(kAttnBlock, waves_per_simd(TYPE, GQ)) void k_attn_r
   }
 }
 
+// ---- long lists of the cache whose query heads share key heads: matrix instructions ----------------------------------------------------
+//
+// A wavefront takes a chunk, one key head and up to eight of its query heads, 32 entries at a time, in two tiles of 16:
+//   scores     S^T = K Q^T, 16 entries by 16 columns, v_mfma_f32_16x16x32_bf16.  A lane (j = lane % 16, b = lane / 16) brings 16-byte pieces of
+//              entry j's key as they lie in memory, piece b of every 64 columns; the order of the columns in the sum is free, so the query's
+//              operand is laid out to match.  8-bit keys, times their scale, are bf16 numbers exactly; so is a query in one part (bf16), two
+//              (fp16) or three (fp32).  Column j is query head j % H, so every head comes 16 / H times.
+//   softmax    the lane that is left with a score holds four consecutive entries (4 b ..) of either tile, which is how the second product wants
+//              its operand: nothing is exchanged but the maximum over b.  Rescaling waits until a maximum grows.
+//   values     O = P V, 16 rows (column j of before) by 16 columns of V, 32 entries deep.  P is a sum of three bf16 numbers, two where H > 5
+//              (2^-27, 2^-18 of it are lost): part j / H of head j % H is row j, so the parts cost no instruction of their own.  The value's
+//              scale is P's.  A lane brings W / 16 bytes of eight entries' values, side by side over j, pairs two entries' bytes with v_perm
+//              and converts.
+// At the end the parts of O are added up through LDS.  It does a quarter of the vector instructions of k_attn_chunks for four heads to a group
+// (chunks of 640,000 entries, 8 key heads of 128, 32 query heads: 380 us there); what bounds it are the requests for rows.
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ unsigned bf16_pair(float a, float b) { return two<DCI_BF16>(a, b); }
+// The leading eight bits of x as bf16 in the upper half; x becomes what they leave (0 of an infinity and of what is no number)
+__device__ __forceinline__ unsigned leading(float& x) {
+  const unsigned u = __float_as_uint(x), h = u & 0xFFFF0000u;
+  if ((u & 0x7F800000u) == 0x7F800000u) {
+    x = 0.f;
+    return u & 0x7FFFFFu ? 0x7FC00000u : h;
+  }
+  x -= __uint_as_float(h);
+  return h;
+}
+// Two neighbouring codes, the lower or the higher two of w, times a power of two
+__device__ __forceinline__ unsigned pair_of_codes(unsigned w, float scale, bool high) {
+  return __builtin_bit_cast(unsigned, high ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, false));
+}
+// What lane I of the 16 has
+template <int I>
+__device__ __forceinline__ int of_lane(int x) {
+  return __builtin_amdgcn_update_dpp(0, x, 0x150 + I, 0xF, 0xF, true);
+}
+template <int I>
+__device__ __forceinline__ float of_lane(float x) {
+  return __int_as_float(of_lane<I>(__float_as_int(x)));
+}
+
+template <int W, int NQ>
+__global__ __launch_bounds__(kAttnBlock, W == 256 ? 2 : 3) void k_attn_groups(const Attn a) {
+  constexpr int kBlocks = W / 64, kSteps = W / 32, kWords = W / 64, kTiles = W / 16;
+  __shared__ float sum[kAttnWaves][16][W + 4];
+  const int lane = lane_id(), j = lane & 15, b4 = lane >> 4, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
+  const unsigned unit = blockIdx.x * kAttnWaves + wave, c = unit / (unsigned)a.passes, pass = unit - c * a.passes;
+  const int kv = (int)pass / a.gq_passes, heads = a.pass_heads, h0 = (int)pass % a.gq_passes * heads;
+  const int parts = heads <= 5 ? 3 : 2, part = j / heads;
+  const bool used = part < parts && h0 + j % heads < a.group;
+  const int head = kv * a.group + min(h0 + j % heads, a.group - 1);
+  const long long n = rows_of(a);
+  if (c >= (unsigned)a.n_chunks || n == 0) return;
+  const long long c0 = (long long)c * a.chunk, c1 = min(c0 + a.chunk, min(a.n_edges, a.indptr[n]));
+  if (c0 >= c1) return;
+  const long long first = row_of(a.indptr, n, c0), last = row_of(a.indptr, n, c1 - 1);
+  const float measure = a.scale * kLog2E;
+  const char *k0 = a.k + kv * W + b4 * 16, *v0 = a.v + kv * W + j * (W / 16), *s0 = reinterpret_cast<const char*>(a.scales + 2 * kv);
+  const unsigned s_stride = 8u * a.kv_heads;
+  for (int piece = 0; piece < (first == last ? 1 : 2); ++piece) {
+    const long long row = piece ? last : first, b = a.indptr[row], e = min(a.indptr[row + 1], b + a.longest);
+    if (e - b <= a.chunk || c0 >= e) continue;
+    const long long e0 = max(b, c0);
+    const int entries = (int)(min(e, c1) - e0);
+    const int* __restrict__ src = a.src + e0;
+    int names = lane < entries ? src[lane] : -1;
+    // the query: what multiplies bytes 8 (s % 2) .. of block s / 2
+    bf16x8 q[NQ][kSteps];
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+      float x[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = 0.f;
+      if (used)
+        read_chunk(a.type, a.q + row * a.q_stride + (long long)(head * a.dim + (s / 2) * 64 + b4 * 16 + (s & 1) * 8) * type_bytes(a.type), 8, true, x);
+#pragma unroll
+      for (int p = 0; p < NQ; ++p) {
+        u32x4 w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = (leading(x[2 * i]) >> 16) | leading(x[2 * i + 1]);
+        q[p][s] = __builtin_bit_cast(bf16x8, w);
+      }
+    }
+    names = named(a, names);
+    float m = -INFINITY, l = 0.f;
+    f32x4 o[kTiles];
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    int names_now = names, source_next = kWave + lane < entries ? src[kWave + lane] : -1;
+    for (int t0 = 0; t0 < entries; t0 += 32) {
+      if (t0 % kWave == 0 && t0) {
+        names_now = named(a, source_next);
+        source_next = t0 + kWave + lane < entries ? src[t0 + kWave + lane] : -1;
+      }
+      const int half = t0 & 32;
+      int at_k[2], at_v = __shfl(names_now, half + ((j & 4) << 2) + b4 * 4 + (j & 3), kWave);  // lane j < 8: entry 4 b + j % 4 of tile j / 4
+      uint4 kc[2][kBlocks];
+      unsigned vc[8][kWords];
+      float ks[2], vs;
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        at_k[t] = max(0, __shfl(names_now, half + t * 16 + j, kWave));
+        const char* p = k0 + (unsigned long long)(unsigned)at_k[t] * a.k_stride;
+#pragma unroll
+        for (int x = 0; x < kBlocks; ++x) kc[t][x] = load_16(p + x * 64);
+        ks[t] = *reinterpret_cast<const float*>(s0 + (unsigned long long)((unsigned)at_k[t] >> a.block_log2) * s_stride);
+      }
+      const bool gone = at_v < 0, any_gone = __any(gone);
+      const int row_v = max(0, at_v);
+      vs = *reinterpret_cast<const float*>(s0 + 4 + (unsigned long long)((unsigned)row_v >> a.block_log2) * s_stride);
+#define DCI_EIGHT(DO_) DO_(0) DO_(1) DO_(2) DO_(3) DO_(4) DO_(5) DO_(6) DO_(7)
+#define DCI_LOAD(I_)                                                                                \
+  {                                                                                                 \
+    const char* p = v0 + (unsigned long long)(unsigned)of_lane<I_>(row_v) * a.v_stride;             \
+    if (kWords == 1) vc[I_][0] = *reinterpret_cast<const unsigned*>(p);                             \
+    else if (kWords == 2) {                                                                         \
+      const uint2 u = *reinterpret_cast<const uint2*>(p);                                           \
+      vc[I_][0] = u.x;                                                                              \
+      vc[I_][kWords > 1 ? 1 : 0] = u.y;                                                             \
+    } else {                                                                                        \
+      const uint4 u = load_16(p);                                                                   \
+      vc[I_][0] = u.x;                                                                              \
+      vc[I_][kWords > 1 ? 1 : 0] = u.y;                                                             \
+      vc[I_][kWords > 2 ? 2 : 0] = u.z;                                                             \
+      vc[I_][kWords > 2 ? 3 : 0] = u.w;                                                             \
+    }                                                                                               \
+  }
+      DCI_EIGHT(DCI_LOAD)
+#undef DCI_LOAD
+      float z[8];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int x = 0; x < kSteps; ++x) {
+          const uint4 w = kc[t][x / 2];
+          const unsigned lo = x & 1 ? w.z : w.x, hi = x & 1 ? w.w : w.y;
+          const u32x4 u = {pair_of_codes(lo, ks[t], false), pair_of_codes(lo, ks[t], true), pair_of_codes(hi, ks[t], false), pair_of_codes(hi, ks[t], true)};
+#pragma unroll
+          for (int p = 0; p < NQ; ++p) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u), q[p][x], s, 0, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) z[4 * t + i] = s[i];
+      }
+      if (any_gone) {
+#define DCI_GONE(I_)                                     \
+  if (of_lane<I_>(at_v) < 0) {                           \
+    z[I_] = -INFINITY;                                   \
+    _Pragma("unroll") for (int x = 0; x < kWords; ++x) vc[I_][x] = 0; \
+  }
+        DCI_EIGHT(DCI_GONE)
+#undef DCI_GONE
+      }
+      if (a.scores && used && part == 0) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int t = t0 + (i >> 2) * 16 + b4 * 4 + (i & 3);
+          if (t < entries) a.scores[(e0 + t) * a.heads + head] = z[i] == -INFINITY ? z[i] : z[i] * a.scale;
+        }
+      }
+      float top = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        z[i] = z[i] == -INFINITY ? z[i] : z[i] * measure;
+        top = fmaxf(top, z[i]);
+      }
+      top = fmaxf(top, __shfl_xor(top, 16, kWave));
+      top = fmaxf(top, __shfl_xor(top, 32, kWave));
+      if (__any(top > m)) {
+        const float next = fmaxf(m, top), shrink = __builtin_amdgcn_exp2f(m - finite_or_0(next));
+        m = next;
+        l *= shrink;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float f = __shfl(shrink, b4 * 4 + r, kWave);
+#pragma unroll
+          for (int i = 0; i < kTiles; ++i) o[i][r] *= f;
+        }
+      }
+      const float base = finite_or_0(m);
+      unsigned pw[4];
+      float p[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        p[i] = __builtin_amdgcn_exp2f(z[i] - base);
+        l += p[i];
+      }
+#define DCI_SCALE(I_) p[I_] *= of_lane<I_>(vs);
+      DCI_EIGHT(DCI_SCALE)
+#undef DCI_SCALE
+#undef DCI_EIGHT
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float x = p[2 * i], y = p[2 * i + 1];
+        unsigned w = bf16_pair(x, y);
+        if (part > 0) {
+          x -= __uint_as_float(w << 16);
+          y -= __uint_as_float(w & 0xFFFF0000u);
+          w = bf16_pair(x, y);
+          if (part > 1) w = bf16_pair(x - __uint_as_float(w << 16), y - __uint_as_float(w & 0xFFFF0000u));
+        }
+        pw[i] = used ? w : 0;
+      }
+      const bf16x8 pa = __builtin_bit_cast(bf16x8, (u32x4{pw[0], pw[1], pw[2], pw[3]}));
+#pragma unroll
+      for (int x = 0; x < kWords; ++x) {
+        unsigned low[4], high[4];  // two entries' bytes 0 0' 1 1', 2 2' 3 3'
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          low[i] = __builtin_amdgcn_perm(vc[2 * i + 1][x], vc[2 * i][x], 0x05010400u);
+          high[i] = __builtin_amdgcn_perm(vc[2 * i + 1][x], vc[2 * i][x], 0x07030602u);
+        }
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+          u32x4 u;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) u[i] = pair_of_codes(d < 2 ? low[i] : high[i], 1.f, d & 1);
+          o[4 * x + d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pa, __builtin_bit_cast(bf16x8, u), o[4 * x + d], 0, 0, 0);
+        }
+      }
+    }
+    l += __shfl_xor(l, 16, kWave);
+    l += __shfl_xor(l, 32, kWave);
+    const long long at0 = (2 * (long long)c + (b > c0 ? 1 : 0)) * a.heads;
+    if (used && part == 0 && b4 == 0) {
+      a.part_ml[2 * (at0 + head)] = m * 0.69314718055994530942f;
+      a.part_ml[2 * (at0 + head) + 1] = l;
+    }
+    // row 4 b + r, columns j (W / 16) + 4 x + d
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+#pragma unroll
+      for (int x = 0; x < kWords; ++x)
+        *reinterpret_cast<float4*>(&sum[wave][b4 * 4 + r][j * (W / 16) + 4 * x]) = make_float4(o[4 * x][r], o[4 * x + 1][r], o[4 * x + 2][r], o[4 * x + 3][r]);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    for (int h = 0; h < heads && h0 + h < a.group; ++h) {
+      for (int col = lane; col < W; col += kWave) {
+        float y = sum[wave][h][col];
+        for (int p = 1; p < parts; ++p) y += sum[wave][h + p * heads][col];
+        a.part_acc[(at0 + kv * a.group + h0 + h) * W + col] = y;
+      }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
 // One workgroup per row and head, or, where there are fewer of them, per chunk and head, for the long list that begins in the chunk: the list's
 // pieces added up in order.  Their weights exp(m - max) are made 256 at a time, in LDS; columns lie side by side, in as many slices of the pieces
 // as the workgroup has room for.
@@ -645,6 +899,7 @@ __global__ __launch_bounds__(kAttnBlock) void k_attn_weights(const Attn a) {
 
 // How a call's work is cut, from its arguments alone (the workspace query has no context)
 struct Split {
+  bool matrix;  // long lists go to k_attn_groups
   int p_log2, lh_log2, wave_heads, gq, gq_passes, passes;
   bool wide;  // heads of 16 bytes at least: read and written 16 at a time
   int chunk;
@@ -653,9 +908,11 @@ struct Split {
 constexpr int64_t kWantedWaves = 4096;  // 16 to a compute unit
 constexpr int kStashHeads = 32;  // query heads of a wavefront, at most, with weights: 40 KB of scores to a workgroup, four workgroups to a compute unit
 
-// cols: columns to a lane; wide: heads are not narrower than a piece.  (The chunks, and so the workspace, do not depend on them.)
-Split split_of(const dci_attn& t, bool accumulate, int cols, bool wide) {
+// type: of k and v
+Split split_of(const dci_attn& t, int type, bool accumulate) {
   Split s;
+  const int cols = type == kE4M3 ? kCols<kE4M3> : kCols<DCI_F32>;
+  const bool wide = t.head_dim * type_bytes(type) >= 16;
   s.wide = wide;
   const int group = t.n_heads / t.kv_heads, gq = group == 1 ? 1 : group == 2 ? 2 : 4;
   s.gq = wide ? gq : 1;
@@ -669,7 +926,8 @@ Split split_of(const dci_attn& t, bool accumulate, int cols, bool wide) {
   s.passes = (t.kv_heads + s.wave_heads - 1) / s.wave_heads * s.gq_passes;
   // chunks of 64 to 512 entries: as long as there are wavefronts enough, 64 lanes of 16 columns each; of 64 with weights, as a wavefront then keeps
   // the scores of the lists that are not cut
-  const int64_t waves = ((int64_t)t.kv_heads * kv_width(t.head_dim) + 1023) / 1024 * ((group + gq - 1) / gq);
+  s.matrix = type == kE4M3 && group >= 3 && !t.bias && (t.head_dim == 64 || t.head_dim == 128 || t.head_dim == 256);
+  const int64_t waves = s.matrix ? (int64_t)t.kv_heads * ((group + 7) / 8) : ((int64_t)t.kv_heads * kv_width(t.head_dim) + 1023) / 1024 * ((group + gq - 1) / gq);
   s.chunk = 64;
   while (!accumulate && s.chunk < 512 && t.n_edges / s.chunk * waves > kWantedWaves) s.chunk *= 2;
   const int64_t longest = t.max_list > 0 && t.max_list < t.n_edges ? t.max_list : t.n_edges;
@@ -743,15 +1001,22 @@ void launch_attn(const Split& s, const Attn& a, unsigned chunk_grid, unsigned ro
   else launch_attn<TYPE, 4, true>(a, chunk_grid, row_grid, lds, stream);
 }
 
+template <int W>
+void launch_groups(const Attn& a, unsigned grid, hipStream_t stream) {
+  if (a.type == DCI_BF16) hipLaunchKernelGGL((k_attn_groups<W, 1>), dim3(grid), dim3(kAttnBlock), 0, stream, a);
+  else if (a.type == DCI_F16) hipLaunchKernelGGL((k_attn_groups<W, 2>), dim3(grid), dim3(kAttnBlock), 0, stream, a);
+  else hipLaunchKernelGGL((k_attn_groups<W, 3>), dim3(grid), dim3(kAttnBlock), 0, stream, a);
+}
+
 int32_t attn(dci_ctx* ctx, const dci_attn& t, int type, Attn a, bool accumulate) {
-  const Split s = split_of(t, accumulate, type == kE4M3 ? kCols<kE4M3> : kCols<DCI_F32>, t.head_dim * type_bytes(type) >= 16);
+  const Split s = split_of(t, type, accumulate);
   Arena ar(ctx->ws, ctx->ws_bytes);
   const Parts parts = take_parts(ar, t, s, accumulate);
   if (!ar.ok()) {
     ctx->req_workspace = ar.off;
     return fail(ctx, DCI_ERR_CAPACITY, "workspace holds %zu bytes, this attention call needs %zu", ctx->ws_bytes, ar.off);
   }
-  if (s.n_chunks * t.n_heads > 0x7FFFFFFFll || s.n_chunks * s.passes > 0x7FFFFFFFll || t.n_rows * s.passes > 0xF0000000ll)
+  if (s.n_chunks * t.n_heads * 4 > 0x7FFFFFFFll || t.n_rows * s.passes > 0xF0000000ll)
     return fail(ctx, DCI_ERR_UNSUPPORTED, "attention: too many list entries and heads for one call");
   const int64_t b = type_bytes(t.dtype);
   a.n_rows = t.n_rows;
@@ -800,11 +1065,25 @@ int32_t attn(dci_ctx* ctx, const dci_attn& t, int type, Attn a, bool accumulate)
   const int64_t at_a_time = (int64_t)ctx->num_cus * waves_per_simd(type, s.gq);
   if (blocks > at_a_time) blocks = at_a_time;
   blocks = (blocks + s.passes - 1) / s.passes * s.passes;  // a wavefront keeps its share of the heads from row to row
-  const unsigned chunk_grid = (unsigned)((s.n_chunks * s.passes + kAttnWaves - 1) / kAttnWaves), row_grid = (unsigned)blocks;
+  unsigned chunk_grid = (unsigned)((s.n_chunks * s.passes + kAttnWaves - 1) / kAttnWaves), row_grid = (unsigned)blocks, group_grid = 0;
+  Attn by_group = a;
+  if (s.matrix && s.n_chunks) {
+    by_group.gq_passes = (a.group + 7) / 8;
+    by_group.pass_heads = (a.group + by_group.gq_passes - 1) / by_group.gq_passes;
+    by_group.passes = t.kv_heads * by_group.gq_passes;
+    group_grid = (unsigned)((s.n_chunks * by_group.passes + kAttnWaves - 1) / kAttnWaves);
+    chunk_grid = 0;
+  }
   const OnDevice on(ctx->device);
   DCI_HIP(ctx, on.err);
   {
     Timed timed(ctx, DCI_K_ATTN);
+    if (group_grid) {
+      if (t.head_dim == 64) launch_groups<64>(by_group, group_grid, ctx->stream);
+      else if (t.head_dim == 128) launch_groups<128>(by_group, group_grid, ctx->stream);
+      else launch_groups<256>(by_group, group_grid, ctx->stream);
+      DCI_LAUNCH_CHECK(ctx);
+    }
     if (type == kE4M3) launch_attn<kE4M3>(s, a, chunk_grid, row_grid, lds, ctx->stream);
     else if (type == DCI_F32) launch_attn<DCI_F32>(s, a, chunk_grid, row_grid, lds, ctx->stream);
     else if (type == DCI_BF16) launch_attn<DCI_BF16>(s, a, chunk_grid, row_grid, lds, ctx->stream);
@@ -830,9 +1109,15 @@ extern "C" {
 
 size_t dci_attn_workspace_bytes(const dci_attn* attn, int32_t accumulate) {
   if (!attn || !dci::sizes_ok(*attn) || attn->n_edges > dci::kMaxEdges) return 0;
-  dci::Arena ar(nullptr, 0);
-  (void)dci::take_parts(ar, *attn, dci::split_of(*attn, accumulate != 0, dci::kChunk, true), accumulate != 0);
-  return ar.off;
+  // for rows of the cache or dense ones, whichever need more
+  size_t most = 0;
+  for (int type : {(int)dci::kE4M3, (int)attn->dtype}) {
+    if (type != dci::kE4M3 && !dci::known_type(type)) return 0;
+    dci::Arena ar(nullptr, 0);
+    (void)dci::take_parts(ar, *attn, dci::split_of(*attn, type, accumulate != 0), accumulate != 0);
+    if (ar.off > most) most = ar.off;
+  }
+  return most;
 }
 
 int32_t dci_attn_forward(dci_ctx* ctx, const dci_attn* attn, const void* k, int64_t k_stride, const void* v, int64_t v_stride) {

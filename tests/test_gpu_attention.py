@@ -131,6 +131,17 @@ def test_cached_long_lists_are_cut_and_joined(heads, kv, dim, dtype, bias_heads)
     cached_case(dci, dci.Context(0), CUT, heads, kv, dim, dtype, seed=dim, bias_heads=bias_heads)
 
 
+# query heads that share key heads, where long lists go through the matrix instructions: three to eight heads at a time, 64, 128 and 256 columns
+@pytest.mark.parametrize("heads,kv,dim,dtype", [
+    (4, 1, 64, "bf16"), (4, 1, 64, "fp16"), (4, 1, 64, "fp32"), (3, 1, 128, "fp32"), (10, 2, 128, "fp16"), (12, 2, 128, "bf16"), (21, 3, 64, "fp32"),
+    (8, 1, 256, "bf16"), (16, 2, 256, "fp32"), (9, 1, 64, "bf16"), (16, 1, 128, "fp16"), (40, 2, 64, "bf16")])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_cached_long_lists_of_shared_key_heads(heads, kv, dim, dtype, accumulate):
+    import paper_2503_01281_amd as dci
+    cached_case(dci, dci.Context(0), CUT, heads, kv, dim, dtype, seed=heads, accumulate=accumulate)
+    cached_case(dci, dci.Context(0), [0, 95, 96, 97, 31, 1, 500], heads, kv, dim, dtype, seed=dim, block=1, by_slot=True, accumulate=accumulate)
+
+
 @pytest.mark.parametrize("lengths", [[1], [0], [64], [65], [0, 0, 3000, 0], [1000] * 3, [70] * 40])
 @pytest.mark.parametrize("accumulate", [False, True])
 def test_cached_few_rows(lengths, accumulate):
@@ -284,6 +295,12 @@ def test_many_entries_take_longer_chunks():
     ctx.sync()
     want = ref.attend(q.astype(np.float64), k.astype(np.float64), v.astype(np.float64), indptr, src.astype(np.int64), 0.25)
     check(out, lse, want, len(lengths), "fp32")
+
+
+def test_many_entries_of_shared_key_heads():
+    import paper_2503_01281_amd as dci
+    lengths = np.array([150_000, 5, 0, 513, 512, 100_001, 511, 64, 63, 1025])
+    cached_case(dci, dci.Context(0), lengths, 4, 1, 64, "bf16", seed=11, n_slots=5_000, accumulate=False)
 
 
 def test_a_side_stream_and_a_graph():
