@@ -517,9 +517,9 @@ typedef struct {
   int32_t bias_heads;      /* 1 (shared by the heads) or n_heads; 0 without bias                       */
 } dci_attn;
 
-/* Workspace of an attention call (accumulate as for dci_attn_cached): lists longer than 64 to 512 entries (the more entries there are in all, the
- * longer) are cut, and their parts joined from there; with accumulate those longer than 64 are, and their scores are kept there.  0 where max_list says that there are no such
- * lists.  It depends on n_rows, n_edges, max_list, heads, head_dim and accumulate only. */
+/* Workspace of an attention call (accumulate as for dci_attn_cached): lists of more than 64 entries are worked on in pieces, which are joined from
+ * there; with accumulate their scores are kept there.  0 where max_list says that there are no such lists.  It depends on n_rows, n_edges,
+ * max_list, dtype, heads, head_dim, bias and accumulate only. */
 size_t dci_attn_workspace_bytes(const dci_attn* attn, int32_t accumulate);
 
 /* Attention over dense rows (a model's later layers): source s, key head h at k + s * k_stride + h * head_dim, v likewise; strides in

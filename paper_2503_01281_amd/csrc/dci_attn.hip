@@ -13,11 +13,10 @@
 //   A group's lanes look up P entries at a time, an entry to a lane, the next P while these are worked on; what an entry names then goes from its
 //   lane to all of them.  An entry that is left out takes row 0's place and a score of -inf.
 //   Query heads that share a key head are worked on together, up to four of them (GQ), from the same registers.
-// Lists longer than `chunk` entries are cut at multiples of it in the whole array of entries, so that neither the number nor the
-// length of lists needs to be known: a wavefront takes `chunk` entries, finds the rows they belong to (a 64-way search in indptr) and
-// leaves (m, l, acc) of its piece of a long list in the workspace.  At most two pieces of long lists meet in a chunk, as a list that lay between
-// two others inside it would be no longer than it: the list that goes on from before (or begins with the chunk) is piece 0, one that begins
-// inside is piece 1.  k_attn_join adds a list's pieces up in order.
+// Lists of more than 64 entries are worked on by chunks: a wavefront takes `chunk` entries of the whole array of entries, so that neither the
+// number nor the length of lists needs to be known, and finds the rows they belong to (a 64-way search in indptr).  A list that lies within a chunk
+// is done there; of others (m, l, acc) of the piece is left in the workspace, for k_attn_join to add up in order.  A chunk has at most two such
+// pieces: that of a list that goes on from before or begins with the chunk (0), and that of one that begins inside and goes on behind it (1).
 // What bounds it: the rows' bytes.  A row of the cache is 2 * kv_heads * head_dim bytes in one place, so a gather of whole rows
 // goes at nearly the rate of a copy.
 #include "dci_kv.h"
@@ -26,6 +25,7 @@ namespace dci {
 namespace {
 
 constexpr int kAttnBlock = 256, kAttnWaves = kAttnBlock / kWave;
+constexpr int kShort = 64;  // longer lists are worked on by chunks
 constexpr float kLog2E = 1.44269504088896340736f;
 // wavefronts to a SIMD that the registers are shared out for: as many as there are without spilling
 constexpr int waves_per_simd(int type, int gq) { return gq == 4 ? 2 : gq == 2 ? 3 : type == DCI_F32 || type == kE4M3 ? 3 : 4; }
@@ -63,12 +63,12 @@ struct Attn {
   int gq_passes;                // of them, those that share a group
   int pass_heads;               // query heads to one of those, in k_attn_groups
   int chunk;
-  int n_chunks;  // 0: no list is cut
+  int n_chunks;  // 0: there are no long lists
   long long longest;  // entries of a list that count
   int stash_row;  // with weights: floats of LDS for the scores of an entry (an odd number, against bank conflicts), 0 without
   float* part_ml;   // [2 n_chunks, heads, 2]
   float* part_acc;  // [2 n_chunks, heads, W]
-  float* all_lse;   // lse of the cut lists by row, accumulating only
+  float* all_lse;   // lse of the long lists by row, accumulating only
 };
 
 // What a lane of an attention wavefront is there for
@@ -98,21 +98,43 @@ struct State {
 
 __device__ __forceinline__ float exp_diff(float a, float b) { return __builtin_amdgcn_exp2f((a - b) * kLog2E); }
 __device__ __forceinline__ float log_of(float x) { return __builtin_amdgcn_logf(x) * 0.69314718055994530942f; }
+__device__ __forceinline__ float lse_of(float m, float l) { return l == 0.f ? -INFINITY : m + log_of(l); }
 __device__ __forceinline__ float finite_or_0(float m) { return m == -INFINITY ? 0.f : m; }
 
-// The last row that begins at or before entry p (so the one that holds it, if one does); n >= 1, wavefront-wide
-__device__ __forceinline__ long long row_of(const long long* __restrict__ indptr, long long n, long long p) {
-  long long lo = 0, hi = n;
-  while (hi - lo > 1) {
-    const long long step = (hi - lo + kWave - 1) / kWave;
-    const long long at = lo + lane_id() * step;
-    const unsigned long long before = __ballot(at < hi && indptr[at] <= p);
-    const int c = __popcll(before);  // a prefix of the lanes, as indptr ascends
-    if (c == 0) return lo;
-    lo += (c - 1) * step;
-    hi = min(hi, lo + step);
+// The last rows that begin at or before entries p and p2 >= p (so those that hold them, if any do); n >= 1, wavefront-wide
+__device__ __forceinline__ void rows_holding(const long long* __restrict__ indptr, long long n, long long p, long long p2, long long* row, long long* row2) {
+  long long lo = 0, hi = n, lo2 = 0, hi2 = n;
+  while (hi - lo > 1 || hi2 - lo2 > 1) {
+    const long long step = (hi - lo + kWave - 1) / kWave, step2 = (hi2 - lo2 + kWave - 1) / kWave;
+    const long long at = lo + lane_id() * step, at2 = lo2 + lane_id() * step2;
+    const bool before = at < hi && indptr[at] <= p, before2 = at2 < hi2 && indptr[at2] <= p2;
+    const int c = __popcll(__ballot(before)), c2 = __popcll(__ballot(before2));  // prefixes of the lanes, as indptr ascends
+    if (c) lo += (c - 1) * step;
+    hi = min(hi, lo + (c ? step : 1));
+    if (c2) lo2 += (c2 - 1) * step2;
+    hi2 = min(hi2, lo2 + (c2 ? step2 : 1));
   }
-  return lo;
+  *row = lo;
+  *row2 = lo2;
+}
+
+// do_piece(row, b, e) for every list [b, e) of more than kShort entries that has some in [c0, c1)
+template <class F>
+__device__ __forceinline__ void for_long_lists(const Attn& a, long long n, long long c0, long long c1, const F& do_piece) {
+  long long first, last;
+  rows_holding(a.indptr, n, c0, c1 - 1, &first, &last);
+  for (long long row0 = first; row0 <= last; row0 += kWave) {
+    const long long row = row0 + lane_id();
+    long long b = 0, e = 0;
+    if (row <= last) {
+      b = a.indptr[row];
+      e = min(min(a.n_edges, a.indptr[row + 1]), b + a.longest);
+    }
+    for (unsigned long long todo = __ballot(b >= 0 && e - b > kShort && e > c0 && b < c1); todo; todo &= todo - 1) {
+      const int i = __builtin_ctzll(todo);
+      do_piece(row0 + i, __shfl(b, i, kWave), __shfl(e, i, kWave));
+    }
+  }
 }
 
 // What entry-holding lane: the row of k and v that source s stands for, -1: none
@@ -404,7 +426,27 @@ __device__ __forceinline__ void write_out(const Attn& a, const Place& pl, char* 
 
 __device__ __forceinline__ long long rows_of(const Attn& a) { return a.n_dev ? min(a.n_rows, max(0ll, *a.n_dev)) : a.n_rows; }
 
-// A chunk to a wavefront: the pieces of up to two long lists, left in the workspace
+// A row's sum is its output
+template <int TYPE, int GQ, bool WIDE>
+__device__ __forceinline__ void finish_row(const Attn& a, const Place& pl, long long row, const State<GQ, kCols<TYPE>>& st) {
+#pragma unroll
+  for (int g = 0; g < GQ; ++g) {
+    if (g < pl.n_q) {
+      const float inv = st.l[g] == 0.f ? 0.f : __builtin_amdgcn_rcpf(st.l[g]);
+      float y[kCols<TYPE>];
+#pragma unroll
+      for (int j = 0; j < kCols<TYPE>; ++j) y[j] = st.acc[g][j] * inv;
+      write_out<TYPE, WIDE>(a, pl, a.out + row * a.out_stride + (long long)((pl.head + g) * a.dim) * type_bytes(a.type), y);
+      if (pl.part == 0) {
+        const float lse = lse_of(st.m[g], st.l[g]);
+        if (a.lse) a.lse[row * a.heads + pl.head + g] = lse;
+        if (a.all_lse) a.all_lse[row * a.heads + pl.head + g] = lse;
+      }
+    }
+  }
+}
+
+// A chunk to a wavefront: what long lists have there
 template <int TYPE, int GQ, bool BIAS, bool WIDE>
 __global__ __launch_bounds__(kAttnBlock, waves_per_simd(TYPE, GQ)) void k_attn_chunks(const Attn a) {
   const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), p_lanes = 1 << a.p_log2;
@@ -415,45 +457,45 @@ __global__ __launch_bounds__(kAttnBlock, waves_per_simd(TYPE, GQ)) void k_attn_c
   if (c >= (unsigned)a.n_chunks || n == 0) return;
   const long long c0 = (long long)c * a.chunk, c1 = min(c0 + a.chunk, min(a.n_edges, a.indptr[n]));
   if (c0 >= c1) return;
-  const long long first = row_of(a.indptr, n, c0), last = row_of(a.indptr, n, c1 - 1);
-  for (int piece = 0; piece < (first == last ? 1 : 2); ++piece) {
-    const long long row = piece ? last : first, b = a.indptr[row], e = min(a.indptr[row + 1], b + a.longest);
-    if (e - b <= a.chunk || c0 >= e) continue;
-    float q[GQ][kCols<TYPE>];
+  for_long_lists(a, n, c0, c1, [&](long long row, long long b, long long e) {
     const int source0 = first_source(a, pl, max(b, c0), min(e, c1), 6 - a.p_log2);
+    float q[GQ][kCols<TYPE>];
     read_q<TYPE, GQ, WIDE>(a, pl, row, true, q);
     State<GQ, kCols<TYPE>> st;
     st.clear();
     (void)attend<TYPE, GQ, BIAS, WIDE>(a, pl, max(b, c0), min(e, c1), 6 - a.p_log2, source0, q, st, nullptr, a.scores);
     for (int apart = p_lanes; apart < kWave; apart <<= 1) join_lanes(st, apart);
-    if (lane_id() < p_lanes) {
+    if (lane_id() >= p_lanes) return;
+    if (b >= c0 && e <= c1) {
+      finish_row<TYPE, GQ, WIDE>(a, pl, row, st);
+      return;
+    }
 #pragma unroll
-      for (int g = 0; g < GQ; ++g) {
-        if (g < pl.n_q) {
-          const long long at = (2 * (long long)c + (b > c0 ? 1 : 0)) * a.heads + pl.head + g;
-          if (pl.part == 0) {
-            a.part_ml[2 * at] = st.m[g];
-            a.part_ml[2 * at + 1] = st.l[g];
-          }
-          float* acc = a.part_acc + at * ((a.dim + kChunk - 1) / kChunk * kChunk);
+    for (int g = 0; g < GQ; ++g) {
+      if (g < pl.n_q) {
+        const long long at = (2 * (long long)c + (b > c0 ? 1 : 0)) * a.heads + pl.head + g;
+        if (pl.part == 0) {
+          a.part_ml[2 * at] = st.m[g];
+          a.part_ml[2 * at + 1] = st.l[g];
+        }
+        float* acc = a.part_acc + at * ((a.dim + kChunk - 1) / kChunk * kChunk);
 #pragma unroll
-          for (int j = 0; j < kPieces<TYPE>; ++j) {
-            bool some;
-            int skip;
-            const int col = first_column<TYPE, WIDE>(a, pl, j, &some, &skip);
-            if (!some) continue;
+        for (int j = 0; j < kPieces<TYPE>; ++j) {
+          bool some;
+          int skip;
+          const int col = first_column<TYPE, WIDE>(a, pl, j, &some, &skip);
+          if (!some) continue;
 #pragma unroll
-            for (int i = 0; i < (WIDE ? kPiece<TYPE> : kCols<TYPE>); i += 4)
-              store_16(reinterpret_cast<char*>(acc + col + i), make_uint4(__float_as_uint(st.acc[g][j * kPiece<TYPE> + i]), __float_as_uint(st.acc[g][j * kPiece<TYPE> + i + 1]),
-                                                                          __float_as_uint(st.acc[g][j * kPiece<TYPE> + i + 2]), __float_as_uint(st.acc[g][j * kPiece<TYPE> + i + 3])));
-          }
+          for (int i = 0; i < (WIDE ? kPiece<TYPE> : kCols<TYPE>); i += 4)
+            store_16(reinterpret_cast<char*>(acc + col + i), make_uint4(__float_as_uint(st.acc[g][j * kPiece<TYPE> + i]), __float_as_uint(st.acc[g][j * kPiece<TYPE> + i + 1]),
+                                                                        __float_as_uint(st.acc[g][j * kPiece<TYPE> + i + 2]), __float_as_uint(st.acc[g][j * kPiece<TYPE> + i + 3])));
         }
       }
     }
-  }
+  });
 }
 
-// Rows, one or more to a wavefront, one set after the other; cut lists are not its business
+// Rows, one or more to a wavefront, one set after the other; long lists are not its business
 template <int TYPE, int GQ, bool BIAS, bool WIDE>
 __global__ __launch_bounds__(kAttnBlock, waves_per_simd(TYPE, GQ)) void k_attn_rows(const Attn a) {
   extern __shared__ float stash_all[];
@@ -475,10 +517,10 @@ __global__ __launch_bounds__(kAttnBlock, waves_per_simd(TYPE, GQ)) void k_attn_r
       *e = a.indptr[row + 1];
     }
   };
-  auto settle = [&](long long* b, long long* e) {  // false for a list that is cut
+  auto settle = [&](long long* b, long long* e) {  // false for a long list
     *b = max(0ll, *b);
     *e = max(*b, min(min(a.n_edges, *e), *b + a.longest));
-    const bool here = !(a.n_chunks && *e - *b > a.chunk);
+    const bool here = !(a.n_chunks && *e - *b > kShort);
     if (!here) *e = *b;
     return here;
   };
@@ -501,25 +543,13 @@ __global__ __launch_bounds__(kAttnBlock, waves_per_simd(TYPE, GQ)) void k_attn_r
     e = next_e;
     source0 = first_source(a, pl, b, e, r_log2);
     for (int apart = p_lanes; apart < p_lanes << r_log2; apart <<= 1) join_lanes(st, apart);
-    float lse[GQ];
-#pragma unroll
-    for (int g = 0; g < GQ; ++g) {
-      lse[g] = st.l[g] == 0.f ? -INFINITY : st.m[g] + log_of(st.l[g]);
-      if (mine && pl.sub == 0 && g < pl.n_q) {
-        const float inv = st.l[g] == 0.f ? 0.f : __builtin_amdgcn_rcpf(st.l[g]);
-        float y[kCols<TYPE>];
-#pragma unroll
-        for (int j = 0; j < kCols<TYPE>; ++j) y[j] = st.acc[g][j] * inv;
-        write_out<TYPE, WIDE>(a, pl, a.out + row * a.out_stride + (long long)((pl.head + g) * a.dim) * type_bytes(a.type), y);
-        if (a.lse && pl.part == 0) a.lse[row * a.heads + pl.head + g] = lse[g];
-      }
-    }
+    if (mine && pl.sub == 0) finish_row<TYPE, GQ, WIDE>(a, pl, row, st);
     if (!a.stash_row) continue;
     float* lses = stash + (kWave + g_id) * a.stash_row;
     if (pl.part == 0) {
 #pragma unroll
       for (int g = 0; g < GQ; ++g)
-        if (g < pl.n_q) lses[pl.local + g] = lse[g];
+        if (g < pl.n_q) lses[pl.local + g] = lse_of(st.m[g], st.l[g]);
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
@@ -601,13 +631,10 @@ __global__ __launch_bounds__(kAttnBlock, W == 256 ? 2 : 3) void k_attn_groups(co
   if (c >= (unsigned)a.n_chunks || n == 0) return;
   const long long c0 = (long long)c * a.chunk, c1 = min(c0 + a.chunk, min(a.n_edges, a.indptr[n]));
   if (c0 >= c1) return;
-  const long long first = row_of(a.indptr, n, c0), last = row_of(a.indptr, n, c1 - 1);
   const float measure = a.scale * kLog2E;
   const char *k0 = a.k + kv * W + b4 * 16, *v0 = a.v + kv * W + j * (W / 16), *s0 = reinterpret_cast<const char*>(a.scales + 2 * kv);
   const unsigned s_stride = 8u * a.kv_heads;
-  for (int piece = 0; piece < (first == last ? 1 : 2); ++piece) {
-    const long long row = piece ? last : first, b = a.indptr[row], e = min(a.indptr[row + 1], b + a.longest);
-    if (e - b <= a.chunk || c0 >= e) continue;
+  for_long_lists(a, n, c0, c1, [&](long long row, long long b, long long e) {
     const long long e0 = max(b, c0);
     const int entries = (int)(min(e, c1) - e0);
     const int* __restrict__ src = a.src + e0;
@@ -769,10 +796,17 @@ __global__ __launch_bounds__(kAttnBlock, W == 256 ? 2 : 3) void k_attn_groups(co
     }
     l += __shfl_xor(l, 16, kWave);
     l += __shfl_xor(l, 32, kWave);
+    const bool whole = b >= c0 && e <= c1;  // the list lies in the chunk
     const long long at0 = (2 * (long long)c + (b > c0 ? 1 : 0)) * a.heads;
+    m *= 0.69314718055994530942f;
     if (used && part == 0 && b4 == 0) {
-      a.part_ml[2 * (at0 + head)] = m * 0.69314718055994530942f;
-      a.part_ml[2 * (at0 + head) + 1] = l;
+      if (whole) {
+        if (a.lse) a.lse[row * a.heads + head] = lse_of(m, l);
+        if (a.all_lse) a.all_lse[row * a.heads + head] = lse_of(m, l);
+      } else {
+        a.part_ml[2 * (at0 + head)] = m;
+        a.part_ml[2 * (at0 + head) + 1] = l;
+      }
     }
     // row 4 b + r, columns j (W / 16) + 4 x + d
 #pragma unroll
@@ -784,23 +818,33 @@ __global__ __launch_bounds__(kAttnBlock, W == 256 ? 2 : 3) void k_attn_groups(co
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
     for (int h = 0; h < heads && h0 + h < a.group; ++h) {
-      for (int col = lane; col < W; col += kWave) {
-        float y = sum[wave][h][col];
-        for (int p = 1; p < parts; ++p) y += sum[wave][h + p * heads][col];
-        a.part_acc[(at0 + kv * a.group + h0 + h) * W + col] = y;
+      const float sum_h = __shfl(l, h, kWave), inv = sum_h == 0.f ? 0.f : __builtin_amdgcn_rcpf(sum_h);
+      const int at_head = kv * a.group + h0 + h;
+      for (int col = lane * 4; col < W; col += kWave * 4) {
+        float4 y = *reinterpret_cast<const float4*>(&sum[wave][h][col]);
+        for (int p = 1; p < parts; ++p) {
+          const float4 x = *reinterpret_cast<const float4*>(&sum[wave][h + p * heads][col]);
+          y = make_float4(y.x + x.x, y.y + x.y, y.z + x.z, y.w + x.w);
+        }
+        if (!whole) {
+          *reinterpret_cast<float4*>(a.part_acc + (at0 + at_head) * W + col) = y;
+        } else {
+          const float out[4] = {y.x * inv, y.y * inv, y.z * inv, y.w * inv};
+          write_chunk(a.type, a.out + row * a.out_stride + (long long)(at_head * W + col) * type_bytes(a.type), 4, false, out);
+        }
       }
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
-  }
+  });
 }
 
-// One workgroup per row and head, or, where there are fewer of them, per chunk and head, for the long list that begins in the chunk: the list's
-// pieces added up in order.  Their weights exp(m - max) are made 256 at a time, in LDS; columns lie side by side, in as many slices of the pieces
-// as the workgroup has room for.
+// One workgroup per row and head, or, where there are fewer of them, per chunk and head, for the long list that begins in the chunk and goes on behind
+// it: the list's pieces added up in order.  Their weights exp(m - max) are made 256 at a time, in LDS; columns lie side by side, in as many slices of
+// the pieces as the workgroup has room for.
 __global__ __launch_bounds__(kAttnBlock) void k_attn_join(const Attn a, bool by_row) {
   const int head = (int)(blockIdx.x % (unsigned)a.heads);
-  const long long n = a.n_dev ? min(a.n_rows, max(0ll, *a.n_dev)) : a.n_rows;
+  const long long n = rows_of(a);
   long long row = blockIdx.x / (unsigned)a.heads;
   if (by_row) {
     if (row >= n) return;
@@ -808,12 +852,13 @@ __global__ __launch_bounds__(kAttnBlock) void k_attn_join(const Attn a, bool by_
     if (n == 0) return;
     const long long c0 = row * a.chunk, c1 = min(c0 + a.chunk, min(a.n_edges, a.indptr[n]));
     if (c0 >= c1) return;
-    row = row_of(a.indptr, n, c1 - 1);
+    rows_holding(a.indptr, n, c1 - 1, c1 - 1, &row, &row);
     if (a.indptr[row] < c0) return;
   }
   const long long b = a.indptr[row], e = min(min(a.n_edges, a.indptr[row + 1]), b + a.longest);
-  if (b < 0 || e - b <= a.chunk) return;
+  if (b < 0 || e - b <= kShort) return;
   const long long c = b / a.chunk;
+  if (c == (e - 1) / a.chunk) return;  // done in its chunk
   const int width = (a.dim + kChunk - 1) / kChunk * kChunk;
   const int pieces = (int)((e - 1) / a.chunk - c) + 1;
   auto place = [&](int k) { return (2 * (c + k) + (k == 0 && b != c * a.chunk ? 1 : 0)) * a.heads + head; };
@@ -865,7 +910,7 @@ __global__ __launch_bounds__(kAttnBlock) void k_attn_join(const Attn a, bool by_
     else *reinterpret_cast<unsigned short*>(o) = (unsigned short)two<DCI_F16>(y, 0.f);
   }
   if (threadIdx.x == 0) {
-    const float lse = l == 0.f ? -INFINITY : m + log_of(l);
+    const float lse = lse_of(m, l);
     if (a.lse) a.lse[row * a.heads + head] = lse;
     if (a.all_lse) a.all_lse[row * a.heads + head] = lse;
   }
@@ -874,16 +919,11 @@ __global__ __launch_bounds__(kAttnBlock) void k_attn_join(const Attn a, bool by_
 // Accumulated weights of the long lists, an entry to a lane
 __global__ __launch_bounds__(kAttnBlock) void k_attn_weights(const Attn a) {
   const long long c = (long long)blockIdx.x * kAttnWaves + threadIdx.x / kWave;
-  const long long n = a.n_dev ? min(a.n_rows, max(0ll, *a.n_dev)) : a.n_rows;
+  const long long n = rows_of(a);
   if (c >= a.n_chunks || n == 0) return;
   const long long c0 = c * a.chunk, c1 = min(c0 + a.chunk, min(a.n_edges, a.indptr[n]));
   if (c0 >= c1) return;
-  const long long first = row_of(a.indptr, n, c0), last = row_of(a.indptr, n, c1 - 1);
-  for (int piece = 0; piece < 2; ++piece) {
-    const long long row = piece ? last : first;
-    if (piece && first == last) break;
-    const long long b = a.indptr[row], e = min(a.indptr[row + 1], b + a.longest);
-    if (e - b <= a.chunk) continue;
+  for_long_lists(a, n, c0, c1, [&](long long row, long long b, long long e) {
     const long long to = min(e, c1);
     for (long long t = max(b, c0) + lane_id(); t < to; t += kWave) {
       float p = 0.f;
@@ -893,9 +933,8 @@ __global__ __launch_bounds__(kAttnBlock) void k_attn_weights(const Attn a) {
       }
       add_weight(a, named(a, a.src[t]), p);
     }
-  }
+  });
 }
-
 
 // How a call's work is cut, from its arguments alone (the workspace query has no context)
 struct Split {
@@ -924,14 +963,13 @@ Split split_of(const dci_attn& t, int type, bool accumulate) {
   s.p_log2 = log2_up((int64_t)s.wave_heads << s.lh_log2);
   if (s.p_log2 < 2) s.p_log2 = 2;  // entries are taken four at a time
   s.passes = (t.kv_heads + s.wave_heads - 1) / s.wave_heads * s.gq_passes;
-  // chunks of 64 to 512 entries: as long as there are wavefronts enough, 64 lanes of 16 columns each; of 64 with weights, as a wavefront then keeps
-  // the scores of the lists that are not cut
+  // chunks of 64 to 512 entries: as long as there are wavefronts enough
   s.matrix = type == kE4M3 && group >= 3 && !t.bias && (t.head_dim == 64 || t.head_dim == 128 || t.head_dim == 256);
   const int64_t waves = s.matrix ? (int64_t)t.kv_heads * ((group + 7) / 8) : ((int64_t)t.kv_heads * kv_width(t.head_dim) + 1023) / 1024 * ((group + gq - 1) / gq);
   s.chunk = 64;
-  while (!accumulate && s.chunk < 512 && t.n_edges / s.chunk * waves > kWantedWaves) s.chunk *= 2;
+  while (s.chunk < 512 && t.n_edges / s.chunk * waves > kWantedWaves) s.chunk *= 2;
   const int64_t longest = t.max_list > 0 && t.max_list < t.n_edges ? t.max_list : t.n_edges;
-  s.n_chunks = longest > s.chunk ? (t.n_edges + s.chunk - 1) / s.chunk : 0;
+  s.n_chunks = longest > kShort ? (t.n_edges + s.chunk - 1) / s.chunk : 0;
   return s;
 }
 
@@ -1055,7 +1093,7 @@ int32_t attn(dci_ctx* ctx, const dci_attn& t, int type, Attn a, bool accumulate)
   // lane groups to a row: one, unless that leaves wavefronts to be had (no more then than there are entries in a list) or, with weights, the scores
   // of the longest list would not all be at hand at its end
   const int groups_log2 = 6 - s.p_log2;
-  const int64_t mean = t.n_edges / t.n_rows, longest = s.n_chunks ? s.chunk : t.max_list > 0 ? t.max_list : t.n_edges;
+  const int64_t mean = t.n_edges / t.n_rows, longest = s.n_chunks ? kShort : t.max_list > 0 ? t.max_list : t.n_edges;
   a.r_log2 = 0;
   while (a.r_log2 < groups_log2 && ((((t.n_rows * s.passes) << a.r_log2 >> groups_log2) < kWantedWaves && (2ll << a.r_log2) <= mean) ||
                                     (accumulate && (1ll << (s.p_log2 + a.r_log2)) < longest)))
