@@ -13,7 +13,7 @@
 //   A group's lanes look up P entries at a time, an entry to a lane, the next P while these are worked on; what an entry names then goes from its
 //   lane to all of them.  An entry that is left out takes row 0's place and a score of -inf.
 //   Query heads that share a key head are worked on together, up to four of them (GQ), from the same registers.
-// Lists of more than 64 entries are worked on by chunks: a wavefront takes `chunk` entries of the whole array of entries, so that neither the
+// Lists of more than 64 entries, and all where there is a handful of them, are worked on by chunks: a wavefront takes `chunk` entries of the whole array of entries, so that neither the
 // number nor the length of lists needs to be known, and finds the rows they belong to (a 64-way search in indptr).  A list that lies within a chunk
 // is done there; of others (m, l, acc) of the piece is left in the workspace, for k_attn_join to add up in order.  A chunk has at most two such
 // pieces: that of a list that goes on from before or begins with the chunk (0), and that of one that begins inside and goes on behind it (1).
@@ -64,6 +64,7 @@ struct Attn {
   int pass_heads;               // query heads to one of those, in k_attn_groups
   int chunk;
   int n_chunks;  // 0: there are no long lists
+  int short_list;  // longer lists are worked on by chunks: kShort, or 0 where all are
   long long longest;  // entries of a list that count
   int stash_row;  // with weights: floats of LDS for the scores of an entry (an odd number, against bank conflicts), 0 without
   float* part_ml;   // [2 n_chunks, heads, 2]
@@ -118,7 +119,7 @@ __device__ __forceinline__ void rows_holding(const long long* __restrict__ indpt
   *row2 = lo2;
 }
 
-// do_piece(row, b, e) for every list [b, e) of more than kShort entries that has some in [c0, c1)
+// do_piece(row, b, e) for every list [b, e) of more than short_list entries that has some in [c0, c1)
 template <class F>
 __device__ __forceinline__ void for_long_lists(const Attn& a, long long n, long long c0, long long c1, const F& do_piece) {
   long long first, last;
@@ -130,7 +131,7 @@ __device__ __forceinline__ void for_long_lists(const Attn& a, long long n, long 
       b = a.indptr[row];
       e = min(min(a.n_edges, a.indptr[row + 1]), b + a.longest);
     }
-    for (unsigned long long todo = __ballot(b >= 0 && e - b > kShort && e > c0 && b < c1); todo; todo &= todo - 1) {
+    for (unsigned long long todo = __ballot(b >= 0 && e - b > a.short_list && e > c0 && b < c1); todo; todo &= todo - 1) {
       const int i = __builtin_ctzll(todo);
       do_piece(row0 + i, __shfl(b, i, kWave), __shfl(e, i, kWave));
     }
@@ -520,7 +521,7 @@ __global__ __launch_bounds__(kAttnBlock, waves_per_simd(TYPE, GQ)) void k_attn_r
   auto settle = [&](long long* b, long long* e) {  // false for a long list
     *b = max(0ll, *b);
     *e = max(*b, min(min(a.n_edges, *e), *b + a.longest));
-    const bool here = !(a.n_chunks && *e - *b > kShort);
+    const bool here = !(a.n_chunks && *e - *b > a.short_list);
     if (!here) *e = *b;
     return here;
   };
@@ -533,6 +534,13 @@ __global__ __launch_bounds__(kAttnBlock, waves_per_simd(TYPE, GQ)) void k_attn_r
     const bool mine = row < n && here;
     long long next_b, next_e;
     bounds(k + step >= k ? k + step : turns, &next_b, &next_e);
+    if (!__any(mine)) {  // long lists only
+      here = settle(&next_b, &next_e);
+      b = next_b;
+      e = next_e;
+      source0 = first_source(a, pl, b, e, r_log2);
+      continue;
+    }
     float q[GQ][kCols<TYPE>];
     read_q<TYPE, GQ, WIDE>(a, pl, row, mine, q);
     State<GQ, kCols<TYPE>> st;
@@ -617,8 +625,18 @@ __device__ __forceinline__ float of_lane(float x) {
   return __int_as_float(of_lane<I>(__float_as_int(x)));
 }
 
+// 32 entries as they come: the bytes that a lane has of their keys and values, the scales, where the values of the entry that it looks up for the 16 are
+template <int W>
+struct GroupStep {
+  uint4 kc[2][W / 64];
+  unsigned vc[8][W / 64];
+  float ks[2], vs;
+  int at_v;
+  bool gone;  // not all of the 32 name something
+};
+
 template <int W, int NQ>
-__global__ __launch_bounds__(kAttnBlock, W == 256 ? 2 : 3) void k_attn_groups(const Attn a) {
+__global__ __launch_bounds__(kAttnBlock, W == 64 ? 3 : 2) void k_attn_groups(const Attn a) {
   constexpr int kBlocks = W / 64, kSteps = W / 32, kWords = W / 64, kTiles = W / 16;
   __shared__ float sum[kAttnWaves][16][W + 4];
   const int lane = lane_id(), j = lane & 15, b4 = lane >> 4, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
@@ -662,66 +680,62 @@ __global__ __launch_bounds__(kAttnBlock, W == 256 ? 2 : 3) void k_attn_groups(co
 #pragma unroll
     for (int i = 0; i < kTiles; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
     int names_now = names, source_next = kWave + lane < entries ? src[kWave + lane] : -1;
-    for (int t0 = 0; t0 < entries; t0 += 32) {
-      if (t0 % kWave == 0 && t0) {
-        names_now = named(a, source_next);
-        source_next = t0 + kWave + lane < entries ? src[t0 + kWave + lane] : -1;
-      }
-      const int half = t0 & 32;
-      int at_k[2], at_v = __shfl(names_now, half + ((j & 4) << 2) + b4 * 4 + (j & 3), kWave);  // lane j < 8: entry 4 b + j % 4 of tile j / 4
-      uint4 kc[2][kBlocks];
-      unsigned vc[8][kWords];
-      float ks[2], vs;
+    // (the next 32 entries' bytes on their way meanwhile would take registers from the third and the second wavefront of a SIMD: 303 -> 326 us)
+    auto load = [&](GroupStep<W>& s, int half) {
+      int at_k[2];
+      s.at_v = __shfl(names_now, half + ((j & 4) << 2) + b4 * 4 + (j & 3), kWave);  // lane j < 8: entry 4 b + j % 4 of tile j / 4
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         at_k[t] = max(0, __shfl(names_now, half + t * 16 + j, kWave));
         const char* p = k0 + (unsigned long long)(unsigned)at_k[t] * a.k_stride;
 #pragma unroll
-        for (int x = 0; x < kBlocks; ++x) kc[t][x] = load_16(p + x * 64);
-        ks[t] = *reinterpret_cast<const float*>(s0 + (unsigned long long)((unsigned)at_k[t] >> a.block_log2) * s_stride);
+        for (int x = 0; x < kBlocks; ++x) s.kc[t][x] = load_16(p + x * 64);
+        s.ks[t] = *reinterpret_cast<const float*>(s0 + (unsigned long long)((unsigned)at_k[t] >> a.block_log2) * s_stride);
       }
-      const bool gone = at_v < 0, any_gone = __any(gone);
-      const int row_v = max(0, at_v);
-      vs = *reinterpret_cast<const float*>(s0 + 4 + (unsigned long long)((unsigned)row_v >> a.block_log2) * s_stride);
+      s.gone = __any(s.at_v < 0);
+      const int row_v = max(0, s.at_v);
+      s.vs = *reinterpret_cast<const float*>(s0 + 4 + (unsigned long long)((unsigned)row_v >> a.block_log2) * s_stride);
 #define DCI_EIGHT(DO_) DO_(0) DO_(1) DO_(2) DO_(3) DO_(4) DO_(5) DO_(6) DO_(7)
 #define DCI_LOAD(I_)                                                                                \
   {                                                                                                 \
     const char* p = v0 + (unsigned long long)(unsigned)of_lane<I_>(row_v) * a.v_stride;             \
-    if (kWords == 1) vc[I_][0] = *reinterpret_cast<const unsigned*>(p);                             \
+    if (kWords == 1) s.vc[I_][0] = *reinterpret_cast<const unsigned*>(p);                             \
     else if (kWords == 2) {                                                                         \
       const uint2 u = *reinterpret_cast<const uint2*>(p);                                           \
-      vc[I_][0] = u.x;                                                                              \
-      vc[I_][kWords > 1 ? 1 : 0] = u.y;                                                             \
+      s.vc[I_][0] = u.x;                                                                              \
+      s.vc[I_][kWords > 1 ? 1 : 0] = u.y;                                                             \
     } else {                                                                                        \
       const uint4 u = load_16(p);                                                                   \
-      vc[I_][0] = u.x;                                                                              \
-      vc[I_][kWords > 1 ? 1 : 0] = u.y;                                                             \
-      vc[I_][kWords > 2 ? 2 : 0] = u.z;                                                             \
-      vc[I_][kWords > 2 ? 3 : 0] = u.w;                                                             \
+      s.vc[I_][0] = u.x;                                                                              \
+      s.vc[I_][kWords > 1 ? 1 : 0] = u.y;                                                             \
+      s.vc[I_][kWords > 2 ? 2 : 0] = u.z;                                                             \
+      s.vc[I_][kWords > 2 ? 3 : 0] = u.w;                                                             \
     }                                                                                               \
   }
       DCI_EIGHT(DCI_LOAD)
 #undef DCI_LOAD
+    };
+    auto work = [&](GroupStep<W>& s, int t0) {
       float z[8];
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        f32x4 s = {0.f, 0.f, 0.f, 0.f};
+        f32x4 sum_t = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int x = 0; x < kSteps; ++x) {
-          const uint4 w = kc[t][x / 2];
+          const uint4 w = s.kc[t][x / 2];
           const unsigned lo = x & 1 ? w.z : w.x, hi = x & 1 ? w.w : w.y;
-          const u32x4 u = {pair_of_codes(lo, ks[t], false), pair_of_codes(lo, ks[t], true), pair_of_codes(hi, ks[t], false), pair_of_codes(hi, ks[t], true)};
+          const u32x4 u = {pair_of_codes(lo, s.ks[t], false), pair_of_codes(lo, s.ks[t], true), pair_of_codes(hi, s.ks[t], false), pair_of_codes(hi, s.ks[t], true)};
 #pragma unroll
-          for (int p = 0; p < NQ; ++p) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u), q[p][x], s, 0, 0, 0);
+          for (int p = 0; p < NQ; ++p) sum_t = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u), q[p][x], sum_t, 0, 0, 0);
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) z[4 * t + i] = s[i];
+        for (int i = 0; i < 4; ++i) z[4 * t + i] = sum_t[i];
       }
-      if (any_gone) {
+      if (s.gone) {
 #define DCI_GONE(I_)                                     \
-  if (of_lane<I_>(at_v) < 0) {                           \
+  if (of_lane<I_>(s.at_v) < 0) {                           \
     z[I_] = -INFINITY;                                   \
-    _Pragma("unroll") for (int x = 0; x < kWords; ++x) vc[I_][x] = 0; \
+    _Pragma("unroll") for (int x = 0; x < kWords; ++x) s.vc[I_][x] = 0; \
   }
         DCI_EIGHT(DCI_GONE)
 #undef DCI_GONE
@@ -760,7 +774,7 @@ __global__ __launch_bounds__(kAttnBlock, W == 256 ? 2 : 3) void k_attn_groups(co
         p[i] = __builtin_amdgcn_exp2f(z[i] - base);
         l += p[i];
       }
-#define DCI_SCALE(I_) p[I_] *= of_lane<I_>(vs);
+#define DCI_SCALE(I_) p[I_] *= of_lane<I_>(s.vs);
       DCI_EIGHT(DCI_SCALE)
 #undef DCI_SCALE
 #undef DCI_EIGHT
@@ -782,8 +796,8 @@ __global__ __launch_bounds__(kAttnBlock, W == 256 ? 2 : 3) void k_attn_groups(co
         unsigned low[4], high[4];  // two entries' bytes 0 0' 1 1', 2 2' 3 3'
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          low[i] = __builtin_amdgcn_perm(vc[2 * i + 1][x], vc[2 * i][x], 0x05010400u);
-          high[i] = __builtin_amdgcn_perm(vc[2 * i + 1][x], vc[2 * i][x], 0x07030602u);
+          low[i] = __builtin_amdgcn_perm(s.vc[2 * i + 1][x], s.vc[2 * i][x], 0x05010400u);
+          high[i] = __builtin_amdgcn_perm(s.vc[2 * i + 1][x], s.vc[2 * i][x], 0x07030602u);
         }
 #pragma unroll
         for (int d = 0; d < 4; ++d) {
@@ -793,6 +807,15 @@ __global__ __launch_bounds__(kAttnBlock, W == 256 ? 2 : 3) void k_attn_groups(co
           o[4 * x + d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pa, __builtin_bit_cast(bf16x8, u), o[4 * x + d], 0, 0, 0);
         }
       }
+    };
+    for (int t0 = 0; t0 < entries; t0 += 32) {
+      if (t0 % kWave == 0 && t0) {
+        names_now = named(a, source_next);
+        source_next = t0 + kWave + lane < entries ? src[t0 + kWave + lane] : -1;
+      }
+      GroupStep<W> s;
+      load(s, t0 & 32);
+      work(s, t0);
     }
     l += __shfl_xor(l, 16, kWave);
     l += __shfl_xor(l, 32, kWave);
@@ -856,13 +879,15 @@ __global__ __launch_bounds__(kAttnBlock) void k_attn_join(const Attn a, bool by_
     if (a.indptr[row] < c0) return;
   }
   const long long b = a.indptr[row], e = min(min(a.n_edges, a.indptr[row + 1]), b + a.longest);
-  if (b < 0 || e - b <= kShort) return;
+  const bool nothing = e <= b && a.short_list == 0;  // no chunk has anything of it
+  if (b < 0 || (e - b <= a.short_list && !nothing)) return;
   const long long c = b / a.chunk;
-  if (c == (e - 1) / a.chunk) return;  // done in its chunk
+  if (!nothing && c == (e - 1) / a.chunk) return;  // done in its chunk
   const int width = (a.dim + kChunk - 1) / kChunk * kChunk;
-  const int pieces = (int)((e - 1) / a.chunk - c) + 1;
+  const int pieces = nothing ? 0 : (int)((e - 1) / a.chunk - c) + 1;
   auto place = [&](int k) { return (2 * (c + k) + (k == 0 && b != c * a.chunk ? 1 : 0)) * a.heads + head; };
-  __shared__ float part[kAttnBlock], red[kAttnWaves], weights[kAttnBlock];
+  __shared__ float4 part[kAttnBlock];
+  __shared__ float red[kAttnWaves], weights[kAttnBlock];
   const int lane = lane_id(), wave = (int)threadIdx.x / kWave;
   float m = -INFINITY;
   for (int k = (int)threadIdx.x; k < pieces; k += kAttnBlock) m = fmaxf(m, a.part_ml[2 * place(k)]);
@@ -872,10 +897,11 @@ __global__ __launch_bounds__(kAttnBlock) void k_attn_join(const Attn a, bool by_
 #pragma unroll
   for (int w = 0; w < kAttnWaves; ++w) m = fmaxf(m, red[w]);
   const float top = finite_or_0(m);
-  int cols = 16;
-  while (cols < width) cols <<= 1;
-  const int slices = kAttnBlock / cols, col = (int)threadIdx.x & (cols - 1), slice = (int)threadIdx.x / cols;
-  float acc = 0.f, l = 0.f;
+  int lanes = 4;  // lanes to a piece, four columns to a lane
+  while (lanes * 4 < width) lanes <<= 1;
+  const int slices = kAttnBlock / lanes, col = ((int)threadIdx.x & (lanes - 1)) * 4, slice = (int)threadIdx.x / lanes;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  float l = 0.f;
   for (int k0 = 0; k0 < pieces; k0 += kAttnBlock) {
     const int k = k0 + (int)threadIdx.x;
     float w = 0.f;
@@ -890,7 +916,11 @@ __global__ __launch_bounds__(kAttnBlock) void k_attn_join(const Attn a, bool by_
     if (col < width) {
       const int end = min(kAttnBlock, pieces - k0);
 #pragma unroll 8
-      for (int i = slice; i < end; i += slices) acc = fmaf(a.part_acc[place(k0 + i) * width + col], weights[i], acc);
+      for (int i = slice; i < end; i += slices) {
+        const float4 x = *reinterpret_cast<const float4*>(a.part_acc + place(k0 + i) * width + col);
+        const float f = weights[i];
+        acc = make_float4(fmaf(x.x, f, acc.x), fmaf(x.y, f, acc.y), fmaf(x.z, f, acc.z), fmaf(x.w, f, acc.w));
+      }
     }
   }
   for (int d = kWave / 2; d; d >>= 1) l += __shfl_xor(l, d, kWave);
@@ -902,12 +932,12 @@ __global__ __launch_bounds__(kAttnBlock) void k_attn_join(const Attn a, bool by_
 #pragma unroll
   for (int w = 0; w < kAttnWaves; ++w) l += red[w];
   if (slice == 0 && col < a.dim) {
-    for (int s = 1; s < slices; ++s) acc += part[s * cols + col];
-    const float y = l == 0.f ? 0.f : acc / l;
-    char* o = a.out + row * a.out_stride + ((long long)head * a.dim + col) * type_bytes(a.type);
-    if (a.type == DCI_F32) *reinterpret_cast<float*>(o) = y;
-    else if (a.type == DCI_BF16) *reinterpret_cast<unsigned short*>(o) = (unsigned short)two<DCI_BF16>(y, 0.f);
-    else *reinterpret_cast<unsigned short*>(o) = (unsigned short)two<DCI_F16>(y, 0.f);
+    for (int s = 1; s < slices; ++s) {
+      const float4 x = part[s * lanes + col / 4];
+      acc = make_float4(acc.x + x.x, acc.y + x.y, acc.z + x.z, acc.w + x.w);
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l, y[4] = {acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv};
+    write_chunk(a.type, a.out + row * a.out_stride + ((long long)head * a.dim + col) * type_bytes(a.type), min(4, a.dim - col), false, y);
   }
   if (threadIdx.x == 0) {
     const float lse = lse_of(m, l);
@@ -1020,11 +1050,10 @@ int32_t check_attn(dci_ctx* ctx, const dci_attn* t) {
   return DCI_OK;
 }
 
-// n_chunks wavefronts' worth of chunks, if there are any, and the rows
 template <int TYPE, int GQ, bool BIAS, bool WIDE>
 void launch_attn(const Attn& a, unsigned chunk_grid, unsigned row_grid, unsigned lds, hipStream_t stream) {
   if (chunk_grid) hipLaunchKernelGGL((k_attn_chunks<TYPE, GQ, BIAS, WIDE>), dim3(chunk_grid), dim3(kAttnBlock), 0, stream, a);
-  hipLaunchKernelGGL((k_attn_rows<TYPE, GQ, BIAS, WIDE>), dim3(row_grid), dim3(kAttnBlock), lds, stream, a);
+  if (row_grid) hipLaunchKernelGGL((k_attn_rows<TYPE, GQ, BIAS, WIDE>), dim3(row_grid), dim3(kAttnBlock), lds, stream, a);
 }
 template <int TYPE, int GQ, bool WIDE>
 void launch_attn(const Attn& a, unsigned chunk_grid, unsigned row_grid, unsigned lds, hipStream_t stream) {
@@ -1090,6 +1119,11 @@ int32_t attn(dci_ctx* ctx, const dci_attn& t, int type, Attn a, bool accumulate)
   a.chunk = s.chunk;
   a.n_chunks = (int)s.n_chunks;
   a.longest = t.max_list > 0 ? t.max_list : t.n_edges;
+  const bool by_row = t.n_rows <= s.n_chunks;
+  // A handful of rows: all by chunks, which spares a launch (305 -> 298 us for 16 long lists), and a row that has nothing is the join's.  With many,
+  // a chunk might hold dozens of tiny lists, and a wavefront takes several microseconds for each.
+  const bool all_by_chunks = by_row && t.n_rows <= 16;
+  a.short_list = all_by_chunks ? 0 : kShort;
   // lane groups to a row: one, unless that leaves wavefronts to be had (no more then than there are entries in a list) or, with weights, the scores
   // of the longest list would not all be at hand at its end
   const int groups_log2 = 6 - s.p_log2;
@@ -1103,7 +1137,7 @@ int32_t attn(dci_ctx* ctx, const dci_attn& t, int type, Attn a, bool accumulate)
   const int64_t at_a_time = (int64_t)ctx->num_cus * waves_per_simd(type, s.gq);
   if (blocks > at_a_time) blocks = at_a_time;
   blocks = (blocks + s.passes - 1) / s.passes * s.passes;  // a wavefront keeps its share of the heads from row to row
-  unsigned chunk_grid = (unsigned)((s.n_chunks * s.passes + kAttnWaves - 1) / kAttnWaves), row_grid = (unsigned)blocks, group_grid = 0;
+  unsigned chunk_grid = (unsigned)((s.n_chunks * s.passes + kAttnWaves - 1) / kAttnWaves), row_grid = all_by_chunks ? 0 : (unsigned)blocks, group_grid = 0;
   Attn by_group = a;
   if (s.matrix && s.n_chunks) {
     by_group.gq_passes = (a.group + 7) / 8;
@@ -1128,7 +1162,6 @@ int32_t attn(dci_ctx* ctx, const dci_attn& t, int type, Attn a, bool accumulate)
     else launch_attn<DCI_F16>(s, a, chunk_grid, row_grid, lds, ctx->stream);
     DCI_LAUNCH_CHECK(ctx);
     if (s.n_chunks) {
-      const bool by_row = t.n_rows <= s.n_chunks;
       hipLaunchKernelGGL(k_attn_join, dim3((unsigned)((by_row ? t.n_rows : s.n_chunks) * t.n_heads)), dim3(kAttnBlock), 0, ctx->stream, a, by_row);
       DCI_LAUNCH_CHECK(ctx);
       if (accumulate) {

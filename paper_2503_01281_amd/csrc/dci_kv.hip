@@ -64,7 +64,8 @@ __device__ __forceinline__ int need_exp(float amax) {
 }
 __device__ __forceinline__ float exp2_of(int e) { return __uint_as_float((unsigned)(e + 127) << 23); }
 
-// 16 numbers as codes, each divided by 2^e first; rounded to nearest even, at most 448
+// 16 numbers as codes, each divided by 2^e first; rounded to nearest even, at most 448.  (The conversion makes NaN of infinities by itself, but of
+// numbers beyond 464 as well, and those only kMaxExp leaves.)
 __device__ __forceinline__ uint4 encode(const float (&x)[kChunk], int e) {
   const float f = exp2_of(-e);
   unsigned w[4];
@@ -73,14 +74,27 @@ __device__ __forceinline__ uint4 encode(const float (&x)[kChunk], int e) {
     float y[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      const float v = x[4 * j + k];
-      y[k] = is_number(v) ? fminf(fmaxf(v * f, -448.f), 448.f) : __uint_as_float(0x7FC00000u);
+      y[k] = x[4 * j + k] * f;
+      if (e == kMaxExp && is_number(y[k])) y[k] = fminf(fmaxf(y[k], -448.f), 448.f);
     }
     int u = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
     u = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], u, true);
     w[j] = (unsigned)u;
   }
   return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// The greatest magnitude among the numbers that are some (infinities are rare, and looked for once one has shown)
+__device__ __forceinline__ float peak_of(const float (&x)[kChunk]) {
+  float amax = 0.f;
+#pragma unroll
+  for (int j = 0; j < kChunk; ++j) amax = fmaxf(amax, fabsf(x[j]));
+  if (!is_number(amax)) {
+    amax = 0.f;
+#pragma unroll
+    for (int j = 0; j < kChunk; ++j) amax = fmaxf(amax, is_number(x[j]) ? fabsf(x[j]) : 0.f);
+  }
+  return amax;
 }
 
 // The block whose entries are rows [i, i + rows) of the list, for one head and kind, by a whole wavefront: first the maximum of what is to be
@@ -103,8 +117,7 @@ __device__ void write_block(const KvWrite& a, int kind, int head, long long i, i
     const int t = t0 + r;
     if (t < rows && cols > 0) {
       read_chunk_as<TYPE>(from + (i + t) * a.stride[kind], cols, a.wide[kind], x);
-#pragma unroll
-      for (int j = 0; j < kChunk; ++j) amax = fmaxf(amax, is_number(x[j]) ? fabsf(x[j]) : 0.f);
+      amax = fmaxf(amax, peak_of(x));
     }
   }
   for (int d = kWave / 2; d; d >>= 1) amax = fmaxf(amax, __shfl_xor(amax, d, kWave));
@@ -148,32 +161,33 @@ __device__ void write_block(const KvWrite& a, int kind, int head, long long i, i
   if (lane == 0) *scale = exp2_of(e);
 }
 
-// A wavefront to `rows` = T * 64 / LH entries of the list (LH lanes to a head of a row, 16 columns each), a key head and a kind (keys or
-// values).  It writes the blocks whose first entry is among its own, whole; the list ascends, so a block's entries are together, and no
-// other wavefront touches this head and kind of the block.  Where a row lies does not depend on its slot, so the rows are on their way while
-// the slots are looked at.  The blocks that end among the wavefront's entries are done side by side, their maxima joined in LDS; one that
-// goes on behind them, and one whose other rows have to be rounded anew, is done on its own (write_block).  What bounds it: the rows' bytes,
-// read and written once.
+// A wavefront to T * 64 / LH entries of the list (LH lanes to a head of a row, 16 columns each) and a key head.  It writes the blocks whose first
+// entry is among its own, whole; the list ascends, so a block's entries are together, and no other wavefront touches this head of the block.  Where
+// a row lies does not depend on its slot, so the rows, keys and values, are on their way while the slots are looked at.  The blocks that end among
+// the wavefront's entries are done side by side, their maxima joined in LDS; one that goes on behind them, and one whose other rows have to be rounded
+// anew, is done on its own (write_block).  What bounds it: the rows' bytes, read and written once.
 template <int TYPE, int T>
 __global__ __launch_bounds__(kKvBlock) void k_kv_write(const KvWrite a) {
-  const int lane = lane_id(), wave = (int)threadIdx.x / kWave;
-  const long long unit = (long long)blockIdx.x * kKvWaves + wave;
-  const int parts = 2 * a.kv_heads;
-  const int kind = (int)(unit % parts) & 1, head = (int)(unit % parts) >> 1;
+  const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
+  const unsigned unit = blockIdx.x * (unsigned)kKvWaves + wave, turn = unit / (unsigned)a.kv_heads;
+  const int head = (int)(unit - turn * a.kv_heads);
   const int lh = 1 << a.lh_log2, at_once = kWave >> a.lh_log2, tile = T * at_once;
-  const long long i0 = unit / parts * tile;
+  const long long i0 = (long long)turn * tile;
   const long long n = a.n_dev ? min(a.n_max, max(0ll, *a.n_dev)) : a.n_max;
-  __shared__ unsigned peaks[kKvWaves][kWave];
+  __shared__ unsigned peaks[kKvWaves][2][kWave];
   if (i0 >= n) return;
   const int r = lane >> a.lh_log2, col = (lane & (lh - 1)) * kChunk, cols = min(kChunk, max(0, a.dim - col));
   const int width = (a.dim + kChunk - 1) / kChunk * kChunk;
-  const char* from = a.from[kind] + ((long long)head * a.dim + col) * type_bytes(TYPE);
-  Chunk<TYPE> x[T];
+  Chunk<TYPE> x[2][T];
 #pragma unroll
-  for (int k = 0; k < T; ++k) {
-    x[k].clear();
-    const long long i = i0 + k * at_once + r;
-    if (i < n && cols > 0) x[k].load(from + i * a.stride[kind], cols, a.wide[kind]);
+  for (int kind = 0; kind < 2; ++kind) {
+    const char* from = a.from[kind] + ((long long)head * a.dim + col) * type_bytes(TYPE);
+#pragma unroll
+    for (int k = 0; k < T; ++k) {
+      x[kind][k].clear();
+      const long long i = i0 + k * at_once + r;
+      if (i < n && cols > 0) x[kind][k].load(from + i * a.stride[kind], cols, a.wide[kind]);
+    }
   }
   auto slot_at = [&](long long i) {
     const int s = i < n ? a.slots[i] : -1;
@@ -182,7 +196,7 @@ __global__ __launch_bounds__(kKvBlock) void k_kv_write(const KvWrite a) {
   const int s = lane < tile ? slot_at(i0 + lane) : -1;
   const int before = i0 + lane > 0 && lane < tile ? slot_at(i0 + lane - 1) : -1;
   const int behind = slot_at(i0 + tile);
-  peaks[wave][lane] = 0;
+  peaks[wave][0][lane] = peaks[wave][1][lane] = 0;
   const bool is_first = s >= 0 && (before < 0 || (before >> a.block_log2) != (s >> a.block_log2));
   if (s >= 0 && i0 + lane > 0 && (before < 0 || before >= s)) *a.host_flag = 2u;  // not ascending: dci_sync says so
   const unsigned long long firsts = __ballot(is_first), real = __ballot(s >= 0);
@@ -198,55 +212,66 @@ __global__ __launch_bounds__(kKvBlock) void k_kv_write(const KvWrite a) {
     const int f = kWave - 1 - __builtin_clzll(up_to);
     return (closed >> f) & 1 ? f : -1;
   };
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
 #pragma unroll
-  for (int k = 0; k < T; ++k) {
-    float amax = 0.f;
+  for (int kind = 0; kind < 2; ++kind) {
 #pragma unroll
-    for (int j = 0; j < kChunk / 2; ++j) {
-      float y, z;
-      x[k].pair(j, y, z);
-      amax = fmaxf(amax, fmaxf(is_number(y) ? fabsf(y) : 0.f, is_number(z) ? fabsf(z) : 0.f));
+    for (int k = 0; k < T; ++k) {
+      float y[kChunk];
+#pragma unroll
+      for (int j = 0; j < kChunk / 2; ++j) x[kind][k].pair(j, y[2 * j], y[2 * j + 1]);
+      const float amax = max_lanes(peak_of(y), a.lh_log2);
+      const int f = first_of(k * at_once + r);
+      if (f >= 0 && col == 0) atomicMax(&peaks[wave][kind][f], __float_as_uint(amax));
     }
-    amax = max_lanes(amax, a.lh_log2);
-    const int f = first_of(k * at_once + r);
-    if (f >= 0 && col == 0) atomicMax(&peaks[wave][f], __float_as_uint(amax));
   }
-  __threadfence_block();
-  // lane f settles the scale of the block that begins with entry f
-  int e = 0;
-  bool apart = false;
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  // lane f settles the scales of the block that begins with entry f
+  int e[2] = {0, 0};
+  bool apart[2] = {false, false};
   if ((closed >> lane) & 1) {
     const unsigned long long later = firsts >> 1 >> lane;
     const int rows = (later ? lane + 1 + __builtin_ctzll(later) : count) - lane;
     const int b = s >> a.block_log2;
     const int block_rows = (int)min(1ll << a.block_log2, a.n_slots - ((long long)b << a.block_log2));
-    float* scale = a.scales + 2 * ((long long)b * a.kv_heads + head) + kind;
-    const float old = *scale;
-    e = need_exp(__uint_as_float(peaks[wave][lane]));
-    if (rows < block_rows && old != 0.f) {
-      const int old_e = (int)(__float_as_uint(old) >> 23) - 127;
-      apart = e > old_e;
-      e = max(e, old_e);
-    }
-    if (!apart) *scale = exp2_of(e);
-  }
-  const unsigned long long alone = __ballot(apart) | (open ? 1ull << last_first : 0ull);
+    float2* scales = reinterpret_cast<float2*>(a.scales) + (long long)b * a.kv_heads + head;
+    float2 now = make_float2(0.f, 0.f);  // a block that is written whole keeps nothing
+    if (rows < block_rows) now = *scales;
 #pragma unroll
-  for (int k = 0; k < T; ++k) {
-    const int row = k * at_once + r, f = first_of(row);
-    const int to_e = __shfl(e, max(f, 0), kWave), to_s = __shfl(s, row, kWave);
-    if (f >= 0 && !((alone >> f) & 1) && col < width) {
-      float y[kChunk];
-#pragma unroll
-      for (int j = 0; j < kChunk / 2; ++j) x[k].pair(j, y[2 * j], y[2 * j + 1]);
-      *reinterpret_cast<uint4*>(a.codes + ((2ll * to_s + kind) * a.kv_heads + head) * width + col) = encode(y, to_e);
+    for (int kind = 0; kind < 2; ++kind) {
+      const float old = kind ? now.y : now.x;
+      e[kind] = need_exp(__uint_as_float(peaks[wave][kind][lane]));
+      if (old != 0.f) {
+        const int old_e = (int)(__float_as_uint(old) >> 23) - 127;
+        apart[kind] = e[kind] > old_e;
+        e[kind] = max(e[kind], old_e);
+      }
     }
+    *scales = make_float2(apart[0] ? now.x : exp2_of(e[0]), apart[1] ? now.y : exp2_of(e[1]));
   }
-  for (unsigned long long todo = alone; todo; todo &= todo - 1) {
-    const long long i = i0 + __builtin_ctzll(todo);
-    int mine = lane < 1 << a.block_log2 ? slot_at(i + lane) : -1;
-    if (mine >= 0 && mine >> a.block_log2 != __shfl(mine, 0, kWave) >> a.block_log2) mine = -1;
-    write_block<TYPE>(a, kind, head, i, mine);
+  const unsigned long long go_on = open ? 1ull << last_first : 0ull;
+#pragma unroll
+  for (int kind = 0; kind < 2; ++kind) {
+    const unsigned long long alone = __ballot(apart[kind]) | go_on;
+#pragma unroll
+    for (int k = 0; k < T; ++k) {
+      const int row = k * at_once + r, f = first_of(row);
+      const int to_e = __shfl(e[kind], max(f, 0), kWave), to_s = __shfl(s, row, kWave);
+      if (f >= 0 && !((alone >> f) & 1) && col < width) {
+        float y[kChunk];
+#pragma unroll
+        for (int j = 0; j < kChunk / 2; ++j) x[kind][k].pair(j, y[2 * j], y[2 * j + 1]);
+        *reinterpret_cast<uint4*>(a.codes + ((2ll * to_s + kind) * a.kv_heads + head) * width + col) = encode(y, to_e);
+      }
+    }
+    for (unsigned long long todo = alone; todo; todo &= todo - 1) {
+      const long long i = i0 + __builtin_ctzll(todo);
+      int mine = lane < 1 << a.block_log2 ? slot_at(i + lane) : -1;
+      if (mine >= 0 && mine >> a.block_log2 != __shfl(mine, 0, kWave) >> a.block_log2) mine = -1;
+      write_block<TYPE>(a, kind, head, i, mine);
+    }
   }
 }
 
@@ -461,7 +486,7 @@ __global__ __launch_bounds__(kAdmitBlock) void k_admit_lookup(const Admit a) {
   if (i >= n) return;
   const long long v = a.nodes[i];
   if (v < 0 || v >= a.num_nodes) return;
-  const int s = __hip_atomic_load(a.remap + v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  const int s = a.remap[v];  // a claim that has just been made may or may not show: either way it is no slot
   if (s >= 0 && (unsigned)s < a.n_slots) atomicOr(a.hit + (s >> 5), 1u << (s & 31));
   else atomicMin(a.remap + v, kClaim + (int)i);
 }
@@ -818,7 +843,7 @@ int32_t dci_kv_write(dci_ctx* ctx, const dci_kv_cache* cache, const int32_t* slo
   const int at_once = dci::kWave >> a.lh_log2;
   int tiles = 1;
   while (tiles < 4 && tiles * at_once < cache->block) tiles *= 2;
-  const int64_t waves = (n_max + tiles * at_once - 1) / (tiles * at_once) * 2 * cache->kv_heads;
+  const int64_t waves = (n_max + tiles * at_once - 1) / (tiles * at_once) * cache->kv_heads;
   const int64_t grid = (waves + dci::kKvWaves - 1) / dci::kKvWaves;
   if (grid > 0x7FFFFFFFll) return dci::fail(ctx, DCI_ERR_UNSUPPORTED, "key/value rows: too many rows and heads for one call");
   dci::Timed timed(ctx, DCI_K_KV);
