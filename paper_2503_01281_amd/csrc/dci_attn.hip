@@ -163,6 +163,24 @@ __device__ __forceinline__ int first_column(const Attn& a, const Place& pl, int 
   *skip = c - col;  // columns that are another piece's
   return col;
 }
+// A lane's columns of a row of the cache, whose heads are padded to whole pieces
+__device__ __forceinline__ int cached_column(const Attn& a, const Place& pl) {
+  return pl.part * kChunk < a.dim ? pl.part * kChunk : 0;
+}
+
+// x[j] = x[j + by], 0 beyond the end (by < 16)
+template <int N>
+__device__ __forceinline__ void shift_down(float (&x)[N], int by) {
+#pragma unroll
+  for (int step = 8; step; step >>= 1) {
+    const bool go = by & step;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const float far = j + step < N ? x[j + step < N ? j + step : j] : 0.f;
+      x[j] = go ? far : x[j];
+    }
+  }
+}
 
 // Entries [e0, e1) that are gone through: none where nothing can be named
 __device__ __forceinline__ int entries(const Attn& a, long long e0, long long e1) {
@@ -195,7 +213,7 @@ __device__ __forceinline__ int attend(const Attn& a, const Place& pl, long long 
   for (int j = 0; j < Chunk<TYPE, C>::kWords; ++j) {
     bool some;
     int skip;
-    offset[j] = first_column<TYPE, WIDE>(a, pl, j, &some, &skip) * type_bytes(TYPE);
+    offset[j] = (TYPE == kE4M3 ? cached_column(a, pl) : first_column<TYPE, WIDE>(a, pl, j, &some, &skip)) * type_bytes(TYPE);
   }
   if (TYPE == kE4M3) {
     k0 += offset[0];
@@ -386,13 +404,17 @@ __device__ __forceinline__ void read_q(const Attn& a, const Place& pl, long long
       const int col = first_column<TYPE, WIDE>(a, pl, j, &some, &skip);
       if (here && some) {
         if (TYPE == kE4M3) {
-          read_chunk(a.type, p + col * type_bytes(a.type), kChunk, true, q[g]);
+          read_chunk(a.type, p + col * type_bytes(a.type), kChunk, true, q[g]);  // columns `skip` before those of the row of the cache
         } else {
           Chunk<TYPE, kPiece<TYPE>> c;
           c.w[0] = load_16(p + col * type_bytes(TYPE));
 #pragma unroll
           for (int i = 0; i < kPiece<TYPE> / 2; ++i) c.pair(i, q[g][j * kPiece<TYPE> + 2 * i], q[g][j * kPiece<TYPE> + 2 * i + 1]);
         }
+      }
+      if (TYPE == kE4M3) {
+        if (a.dim % kChunk) shift_down(q[g], skip & (kChunk - 1));
+        continue;
       }
 #pragma unroll
       for (int i = 0; i < kPiece<TYPE>; ++i)
@@ -413,9 +435,25 @@ __device__ __forceinline__ void write_out(const Attn& a, const Place& pl, char* 
     bool some;
     int skip;
     const int col = first_column<TYPE, WIDE>(a, pl, j, &some, &skip);
-    if (!some) continue;
     if (TYPE == kE4M3) {
-      write_chunk(a.type, p + col * type_bytes(a.type), kChunk, true, y);
+      if (a.dim % kChunk == 0) {
+        if (some) write_chunk(a.type, p + col * type_bytes(a.type), kChunk, true, y);
+        continue;
+      }
+      // the head's last 16 columns: `skip` of the lane before (every lane takes part in the exchange), then its own
+      float both[2 * kChunk];
+#pragma unroll
+      for (int i = 0; i < kChunk; ++i) {
+        both[i] = dpp<0x111>(y[i]);  // of the lane before, in sixteen
+        both[kChunk + i] = y[i];
+      }
+      shift_down(both, (kChunk - skip) & (kChunk - 1));
+      float z[kChunk];
+#pragma unroll
+      for (int i = 0; i < kChunk; ++i) z[i] = skip ? both[i] : y[i];
+      if (some) write_chunk(a.type, p + col * type_bytes(a.type), kChunk, true, z);
+    } else if (!some) {
+      continue;
     } else if (TYPE == DCI_F32) {
       store_16(p + col * 4, make_uint4(__float_as_uint(y[4 * j]), __float_as_uint(y[4 * j + 1]), __float_as_uint(y[4 * j + 2]), __float_as_uint(y[4 * j + 3])));
     } else {
@@ -484,8 +522,9 @@ __global__ __launch_bounds__(kAttnBlock, waves_per_simd(TYPE, GQ)) void k_attn_c
         for (int j = 0; j < kPieces<TYPE>; ++j) {
           bool some;
           int skip;
-          const int col = first_column<TYPE, WIDE>(a, pl, j, &some, &skip);
+          int col = first_column<TYPE, WIDE>(a, pl, j, &some, &skip);
           if (!some) continue;
+          if (TYPE == kE4M3) col = cached_column(a, pl);
 #pragma unroll
           for (int i = 0; i < (WIDE ? kPiece<TYPE> : kCols<TYPE>); i += 4)
             store_16(reinterpret_cast<char*>(acc + col + i), make_uint4(__float_as_uint(st.acc[g][j * kPiece<TYPE> + i]), __float_as_uint(st.acc[g][j * kPiece<TYPE> + i + 1]),
