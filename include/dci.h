@@ -471,7 +471,8 @@ int32_t dci_gather_forward(dci_ctx* ctx, const dci_graph* graph, const dci_cache
  * A slot holds the key and the value row of one node for every key head, as e4m3 codes (sign, four exponent bits, three mantissa
  * bits, no infinities); `block` consecutive slots share a scale per head and kind, a power of two, and a code stands for its value
  * times that scale.  The caller allocates the arrays (device memory) and empties them with dci_kv_clear(); slots are then filled
- * with dci_kv_write(), at places of the caller's own choice or at those that dci_kv_admit() hands out. */
+ * with dci_kv_write(), at places of the caller's own choice or at those that dci_kv_admit() hands out.  Calls on different contexts may read a cache and add
+ * to its weights at the same time; a call that writes rows or gives slots away must not overlap with any other on that cache. */
 typedef struct {
   int64_t n_slots;    /* 1 .. 2^31-1                                                                       */
   int32_t block;      /* slots that share a scale: a power of two, 1 .. 64; the last block may be shorter    */
@@ -492,7 +493,9 @@ typedef struct {
  *   z_e = scale * (q_i . K_e) + bias_e;   p_e = exp(z_e - lse_i);   lse_i = log(sum exp z_e);   out_i = sum p_e V_e.
  * An entry is left out where its bias is -inf or where what it names does not exist (a source outside [0, n_src), a slot outside
  * [0, n_slots)): nothing of its rows is read, whatever they hold.  A row that has nothing left gives out = 0 and lse = -inf.
- * Products, softmax statistics and sums are in fp32; out is rounded once to its type.  Sums run in an order that follows from the
+ * Products, softmax statistics and sums are in fp32; out is rounded once to its type.  (Long lists of the cache whose query heads share key heads,
+ * three or more to one, without bias, of 64, 128 or 256 columns: each weight times its value's scale is a sum of three bf16 numbers, of two where
+ * more than five heads are worked on together, and at most 2^-18 of it is lost, more only where that product is below 2^-100.)  Sums run in an order that follows from the
  * arguments alone, so a call that is made again gives the same bits. */
 typedef struct {
   int64_t n_rows;          /* rows, or their bound where n_dev is given; 0 .. 2^31-1                     */

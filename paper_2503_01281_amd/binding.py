@@ -233,7 +233,14 @@ class Context:
         if rc != 0:
             raise DciError(rc, self.lib.dci_last_error(self._h).decode())
 
+    _captured, _before = False, ()
+
     def ensure_workspace(self, nbytes: int):
+        # A captured graph goes on using the workspace that it was captured with: once there is one, workspaces that are outgrown stay.
+        if torch.cuda.is_initialized() and torch.cuda.is_current_stream_capturing():
+            self._captured = True
+        if self._captured and self._ws is not None and self._ws.numel() - 256 < nbytes:
+            self._before += (self._ws,)
         if self._ws is None or self._ws.numel() - 256 < nbytes:  # (256: for the alignment)
             self.sync()
             self._ws = torch.empty(int(nbytes) + 256, dtype=torch.uint8, device=self.device)

@@ -845,7 +845,7 @@ int32_t dci_kv_write(dci_ctx* ctx, const dci_kv_cache* cache, const int32_t* slo
   while (tiles < 4 && tiles * at_once < cache->block) tiles *= 2;
   const int64_t waves = (n_max + tiles * at_once - 1) / (tiles * at_once) * cache->kv_heads;
   const int64_t grid = (waves + dci::kKvWaves - 1) / dci::kKvWaves;
-  if (grid > 0x7FFFFFFFll) return dci::fail(ctx, DCI_ERR_UNSUPPORTED, "key/value rows: too many rows and heads for one call");
+  if (waves > 0x7FFFFFFFll) return dci::fail(ctx, DCI_ERR_UNSUPPORTED, "key/value rows: too many rows and heads for one call");
   dci::Timed timed(ctx, DCI_K_KV);
   if (dtype == DCI_F32) dci::launch_write<DCI_F32>(tiles, a, (unsigned)grid, ctx->stream);
   else if (dtype == DCI_BF16) dci::launch_write<DCI_BF16>(tiles, a, (unsigned)grid, ctx->stream);

@@ -387,3 +387,40 @@ def test_refusals():
     assert lib.dci_attn_cached(small.handle, C.byref(a), C.byref(cache.c), None, 1) == -2
     assert small.last_required()[2] == lib.dci_attn_workspace_bytes(C.byref(a), 1)
     ctx.sync()
+
+
+def test_a_graph_keeps_the_workspace_it_was_captured_with():
+    """A later call that needs more workspace takes a new one; the graph's own stays, and is nobody else's."""
+    import paper_2503_01281_amd as dci
+    side = torch.cuda.Stream()
+    ctx = dci.Context(0, stream=side)
+    rng = np.random.default_rng(10)
+
+    def inputs(lengths):
+        indptr, src = lists(lengths, 50, rng)
+        return [torch.from_numpy(a).cuda() for a in (indptr, src)] + [torch.randn(len(lengths), 2, 32, device="cuda"), torch.empty(len(lengths), 2, 32, device="cuda")]
+
+    with torch.cuda.stream(side):
+        k, v = torch.randn(50, 2, 32, device="cuda"), torch.randn(50, 2, 32, device="cuda")
+        small, large = inputs([100, 200, 3]), inputs([2000] * 20)
+
+        def call(x):
+            dci.dci_attn_forward(ctx, x[2], k, v, x[0], x[1], x[3], 0.2)
+
+        call(small)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            call(small)
+        held = ctx._ws
+        for replay in range(3):
+            call(large)
+            assert ctx._ws is not held
+            mine = [torch.full((1 << 18,), 3.0, device="cuda") for _ in range(64)]  # what would lie where the old workspace did
+            call(small)
+            ctx.sync()
+            want = small[3].clone()
+            small[3].fill_(float("nan"))
+            torch.cuda.synchronize()
+            graph.replay()
+            ctx.sync()
+            assert torch.equal(small[3], want) and all(bool((m == 3.0).all()) for m in mine), replay
