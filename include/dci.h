@@ -481,8 +481,8 @@ typedef struct {
   uint8_t* codes;     /* [n_slots, 2, kv_heads, W], W = head_dim rounded up to a multiple of 16, the columns behind
                          head_dim zero; keys first, then values; 16-byte aligned                           */
   float* scales;      /* [ceil(n_slots / block), kv_heads, 2]: of keys and of values; 0 = nothing written yet */
-  uint64_t* weight;   /* [n_slots] accumulated attention weight in units of 2^-32; 0 = the slot is free, and a slot
-                         that dci_kv_admit has given away has at least 1                                     */
+  uint64_t* weight;   /* [n_slots] accumulated attention weight in units of 2^-32, below 2^63; 0 = the slot is free,
+                         and a slot that dci_kv_admit has given away has at least 1                          */
   int64_t* node;      /* [n_slots] the node whose rows the slot holds, or -1 (dci_kv_admit)                  */
 } dci_kv_cache;
 

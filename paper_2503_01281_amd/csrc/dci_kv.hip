@@ -392,9 +392,10 @@ int32_t check_rows(dci_ctx* ctx, const dci_kv_cache* cache, const int32_t* slots
 // digit of their highest bits would be the same for all), then digits of 13 bits of the rest, until the slots at the border are all alike or
 // all wanted.  A digit's counts are added up by workgroup in LDS, then in memory; every workgroup of the next kernel looks for the border in them.  Three
 // digits tell weights apart that differ by 2^-33 of themselves (all of them below 16); what is left after that, one workgroup does by itself.
-// Slots and misses are kept as bit masks, numbered by prefix sums over tiles of them, and the j-th slot goes to the j-th miss.
+// Slots and misses are kept as bit masks, numbered by prefix sums over tiles of them, and the j-th slot goes to the j-th miss.  While the call runs, the
+// slots that are hit have the highest bit of their weight set.
 // Nothing waits for another workgroup: what a kernel leaves is looked through by every workgroup of the next (the counts of a digit, the sums of at
-// most 1,024 tiles).  What bounds it: nine launches one after the other, each a few dependent reads long, and 8 bytes per slot and digit that
+// most 1,024 tiles).  What bounds it: seven launches (eight for large caches) one after the other, each a few dependent reads long, and 8 bytes per slot and digit that
 // mostly come from the last-level cache.
 
 constexpr int kDigit = 13, kBins = 1 << kDigit, kDigits = 3;
@@ -429,7 +430,6 @@ struct Admit {
   long long* counts;
   unsigned n_slots;
   AdmitState* st;
-  unsigned* hit;                  // a bit per slot
   unsigned* hist;                 // [kDigits][kBins]
   unsigned* hit_part;             // [kHistBlocks] slots hit
   unsigned long long* node_mask;  // a bit per place of the batch: a miss
@@ -451,7 +451,7 @@ __device__ __forceinline__ unsigned first_digit(unsigned long long w) {
 }
 
 __device__ __forceinline__ long long batch_size(const Admit& a) { return a.n_dev ? min(a.n_max, max(0ll, *a.n_dev)) : a.n_max; }
-__device__ __forceinline__ bool is_hit(const Admit& a, unsigned long long s) { return (a.hit[s >> 5] >> (s & 31)) & 1; }
+constexpr unsigned long long kHit = 1ull << 63;  // in a weight
 
 // Sum of x over the threads before this one, workgroup-wide; total: over all
 template <int BLOCK>
@@ -481,25 +481,28 @@ __device__ unsigned long long tiles_before(const T* tiles, int tile) {
   return total;
 }
 
+// Hits are marked, misses claim their node; and the counts of the digits to come are cleared
 __global__ __launch_bounds__(kAdmitBlock) void k_admit_lookup(const Admit a) {
   const long long n = batch_size(a), i = blockIdx.x * (long long)kAdmitBlock + threadIdx.x;
+  for (long long k = i; k < kDigits * kBins / 4; k += (long long)gridDim.x * kAdmitBlock) reinterpret_cast<uint4*>(a.hist)[k] = make_uint4(0, 0, 0, 0);
   if (i >= n) return;
   const long long v = a.nodes[i];
   if (v < 0 || v >= a.num_nodes) return;
   const int s = a.remap[v];  // a claim that has just been made may or may not show: either way it is no slot
-  if (s >= 0 && (unsigned)s < a.n_slots) atomicOr(a.hit + (s >> 5), 1u << (s & 31));
+  if (s >= 0 && (unsigned)s < a.n_slots) atomicOr(a.weight + s, kHit);
   else atomicMin(a.remap + v, kClaim + (int)i);
 }
 
 // Workgroup-wide: the bin of a digit's counts in which the need-th slot lies.  before: the border after the digit before, nullptr for the first.
+template <int BLOCK>
 __device__ Border find_border(const unsigned* hist, unsigned need, const Border* before) {
-  constexpr int kPer = kBins / kDigitBlock;
+  constexpr int kPer = kBins / BLOCK;
   __shared__ Border found;
   unsigned x[kPer], sum = 0;
 #pragma unroll
   for (int k = 0; k < kPer; ++k) sum += x[k] = hist[threadIdx.x * kPer + k];
   unsigned long long total;
-  unsigned smaller = (unsigned)block_before<kDigitBlock>(sum, &total);
+  unsigned smaller = (unsigned)block_before<BLOCK>(sum, &total);
   if (need == 0) {  // nothing is wanted: no weight is below 0, and none of those that are 0 is needed
     if (threadIdx.x == 0) found = Border{0, 0, 0, 1};
   } else if (smaller < need && smaller + sum >= need) {  // one lane
@@ -537,17 +540,16 @@ __device__ unsigned count_digit(const Admit& a, unsigned* bins, unsigned long lo
   unsigned hits = 0;
   for (unsigned long long s = s0; s < a.n_slots; s += step * kDigitSlots) {
     unsigned long long w[kDigitSlots];
-    bool hit[kDigitSlots], real[kDigitSlots];
+    bool real[kDigitSlots];
 #pragma unroll
     for (int k = 0; k < kDigitSlots; ++k) {
       const unsigned long long at = s + k * step;
       real[k] = at < a.n_slots;
       w[k] = real[k] ? a.weight[at] : 0;
-      hit[k] = real[k] && is_hit(a, at);
     }
 #pragma unroll
     for (int k = 0; k < kDigitSlots; ++k) {
-      if (hit[k]) ++hits;
+      if (w[k] & kHit) ++hits;
       else if (real[k]) {
         if (FIRST) atomicAdd(&bins[first_digit(w[k])], 1u);
         else if (w[k] >> shift == prefix) atomicAdd(&bins[(unsigned)(w[k] >> low) & mask], 1u);
@@ -594,7 +596,7 @@ __device__ Border first_border(const Admit& a) {
   const unsigned misses = (unsigned)tiles_before<kDigitBlock>(a.node_tile, a.node_tiles);
   const unsigned hits = (unsigned)tiles_before<kDigitBlock>(a.hit_part, a.hist_blocks);
   const unsigned want = min(misses, a.n_slots - hits);
-  const Border b = find_border(a.hist, want, nullptr);
+  const Border b = find_border<kDigitBlock>(a.hist, want, nullptr);
   if (blockIdx.x == 0 && threadIdx.x == 0) {
     a.st->misses = misses;
     a.st->hits = hits;
@@ -612,7 +614,7 @@ __global__ __launch_bounds__(kDigitBlock) void k_admit_digit(const Admit a, int 
     b = first_border(a);
   } else {
     b = a.st->border[0];
-    if (!b.done) b = find_border(a.hist + kBins, b.need, &a.st->border[0]);
+    if (!b.done) b = find_border<kDigitBlock>(a.hist + kBins, b.need, &a.st->border[0]);
     if (blockIdx.x == 0 && threadIdx.x == 0) a.st->border[1] = b;
   }
   if (b.done) return;
@@ -624,28 +626,40 @@ __global__ __launch_bounds__(kDigitBlock) void k_admit_digit(const Admit a, int 
     if (bins[k]) atomicAdd(a.hist + digit * kBins + k, bins[k]);
 }
 
-// One workgroup: the border after all digits
-__global__ __launch_bounds__(kDigitBlock) void k_admit_border(const Admit a) {
-  __shared__ unsigned bins[kBins];
+// Workgroup-wide: the border after all digits
+template <int BLOCK>
+__device__ Border last_border(const Admit& a, unsigned* bins) {
   __shared__ Border last;
   Border b = a.st->border[1];
-  if (!b.done) b = find_border(a.hist + 2 * kBins, b.need, &a.st->border[1]);
+  if (!b.done) b = find_border<BLOCK>(a.hist + 2 * kBins, b.need, &a.st->border[1]);
   while (!b.done) {
     if (threadIdx.x == 0) last = b;
-    for (int k = (int)threadIdx.x; k < kBins; k += kDigitBlock) bins[k] = 0;
+    for (int k = (int)threadIdx.x; k < kBins; k += BLOCK) bins[k] = 0;
     __syncthreads();
-    (void)count_digit<false>(a, bins, threadIdx.x, kDigitBlock, b.prefix, b.shift);
+    (void)count_digit<false>(a, bins, threadIdx.x, BLOCK, b.prefix, b.shift);
     __syncthreads();
-    b = find_border(bins, b.need, &last);
+    b = find_border<BLOCK>(bins, b.need, &last);
   }
+  return b;
+}
+
+__global__ __launch_bounds__(kDigitBlock) void k_admit_border(const Admit a) {
+  __shared__ unsigned bins[kBins];
+  const Border b = last_border<kDigitBlock>(a, bins);
   if (threadIdx.x == 0) a.st->border[2] = b;
 }
 
-// Marks the slots below and at the border, and writes the list of the misses that get a slot
+// Marks the slots below and at the border, and writes the list of the misses that get a slot.  FIND: every workgroup looks for the border itself, which
+// spares a launch (3 us); where digits are left over after all, each of them goes through all slots, so only for caches of up to kFindSlots, and
+// the marks of hits stay until nobody looks for it any more (beyond, they are taken off here, in order: k_admit_slots takes twice as long with that).
+constexpr int64_t kFindSlots = 1 << 18;
+template <bool FIND>
 __global__ __launch_bounds__(kAdmitBlock) void k_admit_number(const Admit a) {
+  __shared__ unsigned bins[FIND ? kBins : 1];
   const unsigned want = a.st->want;
   if ((int)blockIdx.x < a.slot_tiles) {
-    const Border b = a.st->border[2];
+    const Border b = FIND ? last_border<kAdmitBlock>(a, bins) : a.st->border[2];
+    if (FIND && blockIdx.x == 0 && threadIdx.x == 0) a.st->border[2] = b;
     unsigned long long sum = 0, total;
     for (int stretch = 0; stretch < a.slot_tile_stretches; ++stretch) {
       const unsigned long long s0 = ((unsigned long long)blockIdx.x * a.slot_tile_stretches + stretch) * kStretch + threadIdx.x;
@@ -654,9 +668,10 @@ __global__ __launch_bounds__(kAdmitBlock) void k_admit_number(const Admit a) {
 #pragma unroll
       for (int k = 0; k < kStretch / kAdmitBlock; ++k) {
         const unsigned long long s = s0 + k * kAdmitBlock;
-        open[k] = s < a.n_slots && want;
-        p[k] = open[k] ? a.weight[s] >> b.shift : 0;
-        open[k] = open[k] && !is_hit(a, s);
+        const unsigned long long w = s < a.n_slots ? a.weight[s] : 0;
+        if (!FIND && (w & kHit)) a.weight[s] = w & ~kHit;
+        open[k] = s < a.n_slots && want && !(w & kHit);
+        p[k] = w >> b.shift;
       }
 #pragma unroll
       for (int k = 0; k < kStretch / kAdmitBlock; ++k) {
@@ -740,7 +755,8 @@ __global__ __launch_bounds__(kAdmitBlock) void k_admit_give(const Admit a) {
   if (threadIdx.x == 0) a.gone_tile[blockIdx.x] = (unsigned)total;
 }
 
-// The slots of the batch; claims that got none are taken back
+// The slots of the batch; claims that got none are taken back, and marks of hits that are still there
+template <bool UNMARK>
 __global__ __launch_bounds__(kAdmitBlock) void k_admit_slots(const Admit a) {
   const long long n = batch_size(a), i = blockIdx.x * (long long)kAdmitBlock + threadIdx.x;
   if (blockIdx.x == 0) {
@@ -758,17 +774,17 @@ __global__ __launch_bounds__(kAdmitBlock) void k_admit_slots(const Admit a) {
   if (v >= 0 && v < a.num_nodes) {
     s = a.remap[v];
     if (s == kClaim + (int)i) a.remap[v] = -1;
-    if (s < 0) s = -1;
+    if (s < 0 || (unsigned)s >= a.n_slots) s = -1;
+    else if (UNMARK) a.weight[s] &= ~kHit;  // (whoever else has the node writes the same)
   }
   a.slots[i] = s;
 }
 
 struct AdmitSpace {
   AdmitState* st;
-  unsigned *hist, *hit, *hit_part, *node_tile, *gone_tile;
+  unsigned *hist, *hit_part, *node_tile, *gone_tile;
   unsigned long long *node_mask, *slot_mask, *slot_tile;
   int node_tiles, node_tile_blocks, slot_tiles, slot_tile_stretches;
-  size_t clear_bytes;  // from hist on
 };
 AdmitSpace admit_space(Arena& ar, int64_t n_slots, int64_t n_max) {
   AdmitSpace s;
@@ -778,8 +794,6 @@ AdmitSpace admit_space(Arena& ar, int64_t n_slots, int64_t n_max) {
   s.slot_tile_stretches = (int)((stretches + kTiles - 1) / kTiles);
   s.slot_tiles = (int)((stretches + s.slot_tile_stretches - 1) / s.slot_tile_stretches);
   s.hist = ar.take<unsigned>((size_t)kDigits * kBins);
-  s.hit = ar.take<unsigned>((size_t)(n_slots + 31) / 32);
-  s.clear_bytes = ar.off;
   s.st = ar.take<AdmitState>(1);
   s.hit_part = ar.take<unsigned>(kHistBlocks);
   s.node_mask = ar.take<unsigned long long>((size_t)s.node_tiles * s.node_tile_blocks * (kDigitBlock / 64));
@@ -929,7 +943,6 @@ int32_t dci_kv_admit(dci_ctx* ctx, const dci_kv_cache* cache, int32_t* remap, in
   a.counts = reinterpret_cast<long long*>(counts);
   a.n_slots = (unsigned)cache->n_slots;
   a.st = sp.st;
-  a.hit = sp.hit;
   a.hist = sp.hist;
   a.hit_part = sp.hit_part;
   a.node_mask = sp.node_mask;
@@ -946,21 +959,25 @@ int32_t dci_kv_admit(dci_ctx* ctx, const dci_kv_cache* cache, int32_t* remap, in
   if (a.hist_blocks > dci::kHistBlocks) a.hist_blocks = dci::kHistBlocks;
   const unsigned node_blocks = (unsigned)(n_max > 0 ? (n_max + dci::kAdmitBlock - 1) / dci::kAdmitBlock : 1);
   dci::Timed timed(ctx, DCI_K_KV);
-  const int32_t filled = dci::fill_bytes(ctx, sp.hist, sp.clear_bytes, 0);
-  if (filled != DCI_OK) return filled;
 #define DCI_ADMIT(kernel_, grid_, block_, ...)                                                                               \
   do {                                                                                                                       \
     hipLaunchKernelGGL(kernel_, dim3((unsigned)(grid_)), dim3(block_), 0, ctx->stream, ##__VA_ARGS__);                       \
     DCI_LAUNCH_CHECK(ctx);                                                                                                   \
   } while (0)
-  DCI_ADMIT(dci::k_admit_lookup, node_blocks, dci::kAdmitBlock, a);
+  DCI_ADMIT(dci::k_admit_lookup, node_blocks < 24 ? 24 : node_blocks, dci::kAdmitBlock, a);
   DCI_ADMIT(dci::k_admit_first_digit, a.hist_blocks + a.node_tiles, dci::kDigitBlock, a);
   DCI_ADMIT(dci::k_admit_digit, a.hist_blocks, dci::kDigitBlock, a, 1);
   DCI_ADMIT(dci::k_admit_digit, a.hist_blocks, dci::kDigitBlock, a, 2);
-  DCI_ADMIT(dci::k_admit_border, 1, dci::kDigitBlock, a);
-  DCI_ADMIT(dci::k_admit_number, a.slot_tiles + (n_max + dci::kDigitBlock - 1) / dci::kDigitBlock, dci::kAdmitBlock, a);
+  const int64_t number_blocks = a.slot_tiles + (n_max + dci::kDigitBlock - 1) / dci::kDigitBlock;
+  if (cache->n_slots <= dci::kFindSlots) {
+    DCI_ADMIT(dci::k_admit_number<true>, number_blocks, dci::kAdmitBlock, a);
+  } else {
+    DCI_ADMIT(dci::k_admit_border, 1, dci::kDigitBlock, a);
+    DCI_ADMIT(dci::k_admit_number<false>, number_blocks, dci::kAdmitBlock, a);
+  }
   DCI_ADMIT(dci::k_admit_give, a.slot_tiles, dci::kAdmitBlock, a);
-  DCI_ADMIT(dci::k_admit_slots, node_blocks, dci::kAdmitBlock, a);
+  if (cache->n_slots <= dci::kFindSlots) DCI_ADMIT(dci::k_admit_slots<true>, node_blocks, dci::kAdmitBlock, a);
+  else DCI_ADMIT(dci::k_admit_slots<false>, node_blocks, dci::kAdmitBlock, a);
 #undef DCI_ADMIT
   return DCI_OK;
 }
