@@ -1013,7 +1013,7 @@ struct Split {
   int chunk;
   int64_t n_chunks;
 };
-constexpr int64_t kWantedWaves = 4096;  // 16 to a compute unit
+constexpr int64_t kWantedWaves = 4096, kFewWaves = 1024;  // 16 and four to a compute unit
 constexpr int kStashHeads = 32;  // query heads of a wavefront, at most, with weights: 40 KB of scores to a workgroup, four workgroups to a compute unit
 
 // type: of k and v
@@ -1032,11 +1032,13 @@ Split split_of(const dci_attn& t, int type, bool accumulate) {
   s.p_log2 = log2_up((int64_t)s.wave_heads << s.lh_log2);
   if (s.p_log2 < 2) s.p_log2 = 2;  // entries are taken four at a time
   s.passes = (t.kv_heads + s.wave_heads - 1) / s.wave_heads * s.gq_passes;
-  // chunks of 64 to 512 entries: as long as there are wavefronts enough
+  // chunks of 64 to 512 entries: as long as there are wavefronts enough.  Shorter ones (16 or 32; a step of k_attn_groups is 32 entries) where that leaves
+  // only a few to a compute unit: 28,000 entries of seven 32-bit heads of 64 take 48 us in chunks of 32 and 55 in chunks of 64.  With more wavefronts
+  // the pieces cost more than they give: 37,000 entries of eight 16-bit heads of 128 on two take 46 us in chunks of 16, 38 in 32, 37 in 64.
   s.matrix = type == kE4M3 && group >= 3 && !t.bias && (t.head_dim == 64 || t.head_dim == 128 || t.head_dim == 256);
   const int64_t waves = s.matrix ? (int64_t)t.kv_heads * ((group + 7) / 8) : ((int64_t)t.kv_heads * kv_width(t.head_dim) + 1023) / 1024 * ((group + gq - 1) / gq);
-  s.chunk = 64;
-  while (s.chunk < 512 && t.n_edges / s.chunk * waves > kWantedWaves) s.chunk *= 2;
+  s.chunk = s.matrix ? 32 : 16;
+  while (s.chunk < 512 && t.n_edges / s.chunk * waves > (s.chunk < 64 ? kFewWaves : kWantedWaves)) s.chunk *= 2;
   const int64_t longest = t.max_list > 0 && t.max_list < t.n_edges ? t.max_list : t.n_edges;
   s.n_chunks = longest > kShort ? (t.n_edges + s.chunk - 1) / s.chunk : 0;
   return s;
