@@ -471,8 +471,10 @@ int32_t dci_gather_forward(dci_ctx* ctx, const dci_graph* graph, const dci_cache
  * A slot holds the key and the value row of one node for every key head, as e4m3 codes (sign, four exponent bits, three mantissa
  * bits, no infinities); `block` consecutive slots share a scale per head and kind, a power of two, and a code stands for its value
  * times that scale.  The caller allocates the arrays (device memory) and empties them with dci_kv_clear(); slots are then filled
- * with dci_kv_write(), at places of the caller's own choice or at those that dci_kv_admit() hands out.  Calls on different contexts may read a cache and add
- * to its weights at the same time; a call that writes rows or gives slots away must not overlap with any other on that cache. */
+ * with dci_kv_write(), at places of the caller's own choice or at those that dci_kv_admit() hands out.  Calls on different contexts
+ * may read a cache and add to its weights at the same time; a call that writes rows or gives slots away must not overlap with any
+ * other on that cache.  A weight only grows while its node stays: a program that runs for long, or wants recent use to count for
+ * more, scales the weights down now and then (those of slots in use to no less than 1). */
 typedef struct {
   int64_t n_slots;    /* 1 .. 2^31-1                                                                       */
   int32_t block;      /* slots that share a scale: a power of two, 1 .. 64; the last block may be shorter    */
@@ -493,10 +495,11 @@ typedef struct {
  *   z_e = scale * (q_i . K_e) + bias_e;   p_e = exp(z_e - lse_i);   lse_i = log(sum exp z_e);   out_i = sum p_e V_e.
  * An entry is left out where its bias is -inf or where what it names does not exist (a source outside [0, n_src), a slot outside
  * [0, n_slots)): nothing of its rows is read, whatever they hold.  A row that has nothing left gives out = 0 and lse = -inf.
- * Products, softmax statistics and sums are in fp32; out is rounded once to its type.  (Long lists of the cache whose query heads share key heads,
- * three or more to one, without bias, of 64, 128 or 256 columns: each weight times its value's scale is a sum of three bf16 numbers, of two where
- * more than five heads are worked on together, and at most 2^-18 of it is lost, more only where that product is below 2^-100.)  Sums run in an order that follows from the
- * arguments alone, so a call that is made again gives the same bits. */
+ * Products, softmax statistics and sums are in fp32; out is rounded once to its type.  (Long lists of the cache whose query heads
+ * share key heads, three or more to one, without bias, of 64, 128 or 256 columns: each weight times its value's scale is a sum of
+ * three bf16 numbers, of two where more than five heads are worked on together, and at most 2^-18 of it is lost, more only where
+ * that product is below 2^-100.)  Sums run in an order that follows from the arguments alone, so a call that is made again gives
+ * the same bits. */
 typedef struct {
   int64_t n_rows;          /* rows, or their bound where n_dev is given; 0 .. 2^31-1                     */
   const int64_t* n_dev;    /* device: the number of rows (nullable); rows from there on are left as they are */
@@ -520,9 +523,9 @@ typedef struct {
   int32_t bias_heads;      /* 1 (shared by the heads) or n_heads; 0 without bias                       */
 } dci_attn;
 
-/* Workspace of an attention call (accumulate as for dci_attn_cached): lists of more than 64 entries are worked on in pieces, which are joined from
- * there; with accumulate their scores are kept there.  0 where max_list says that there are no such lists.  It depends on n_rows, n_edges,
- * max_list, dtype, heads, head_dim, bias and accumulate only. */
+/* Workspace of an attention call (accumulate as for dci_attn_cached): lists of more than 64 entries are worked on in pieces, which
+ * are joined from there; with accumulate their scores are kept there.  0 where max_list says that there are no such lists.  It
+ * depends on n_rows, n_edges, max_list, dtype, heads, head_dim, bias and accumulate only. */
 size_t dci_attn_workspace_bytes(const dci_attn* attn, int32_t accumulate);
 
 /* Attention over dense rows (a model's later layers): source s, key head h at k + s * k_stride + h * head_dim, v likewise; strides in
@@ -530,17 +533,19 @@ size_t dci_attn_workspace_bytes(const dci_attn* attn, int32_t accumulate);
 int32_t dci_attn_forward(dci_ctx* ctx, const dci_attn* attn, const void* k, int64_t k_stride, const void* v, int64_t v_stride);
 
 /* Attention over rows of the cache.  slots: device int32 [n_src], the slot of every source (as dci_kv_admit writes them for
- * blocks->nodes), -1 for none; NULL: src holds slots, and n_src is not used.  accumulate != 0: cache->weight[s] += sum of p_e over the entries that name slot s, the
- * rows and the heads.  An entry's sum over the heads is taken in fp32 (in parts, where there are many heads) and rounded to 2^-32; the additions
- * are of integers, so their order does not matter.  A NaN adds nothing.  head_dim and kv_heads must be the cache's. */
+ * blocks->nodes), -1 for none; NULL: src holds slots, and n_src is not used.  accumulate != 0: cache->weight[s] += sum of p_e over
+ * the entries that name slot s, the rows and the heads.  An entry's sum over the heads is taken in fp32 (in parts, where there are
+ * many heads) and rounded to 2^-32; the additions are of integers, so their order does not matter.  A NaN adds nothing.  head_dim
+ * and kv_heads must be the cache's. */
 int32_t dci_attn_cached(dci_ctx* ctx, const dci_attn* attn, const dci_kv_cache* cache, const int32_t* slots, int32_t accumulate);
 
 /* Empties the cache: scales, weights and codes 0, nodes -1 (weight and node may be NULL). */
 int32_t dci_kv_clear(dci_ctx* ctx, const dci_kv_cache* cache);
 
 /* Writes rows of keys and values into the cache.  slots: device int32 [n_max], STRICTLY ASCENDING; entries outside [0, n_slots) are
- * skipped, with their rows, and stand behind all others (fresh_slots of dci_kv_admit ends in such entries).  The number of rows is *n_dev (device
- * int64) where n_dev is not NULL, n_max its bound.  k, v: device rows of `dtype`, row i, head h at i * stride + h * head_dim.
+ * skipped, with their rows, and stand behind all others (fresh_slots of dci_kv_admit ends in such entries).  The number of rows is
+ * *n_dev (device int64) where n_dev is not NULL, n_max its bound.  k, v: device rows of `dtype`, row i, head h at i * stride + h *
+ * head_dim.
  * For every block that the call writes to, head and kind: need = the least e with max |x| <= 448 * 2^e over the finite numbers written,
  * within [-100, 119]; the block's scale becomes 2^need where the call writes every slot of the block or its scale is 0, and
  * 2^max(need, old) otherwise.  Numbers are divided by the scale and rounded to the nearest e4m3 (ties to even; beyond 448 to
@@ -561,8 +566,8 @@ int32_t dci_kv_read(dci_ctx* ctx, const dci_kv_cache* cache, const int32_t* slot
  * blocks->nodes; a node may appear more than once, ids outside [0, num_nodes) are left alone (slot -1).
  *   1. A node that has a slot keeps it (a hit): the slots of a call's own nodes are not taken away.
  *   2. Every node without one, once, in the order of first appearance, is a miss.  The m = min(misses, slots that are not hit)
- *      slots of least (weight, slot) among those not hit are given to the first m misses, in ascending order; free slots have weight 0 and so
- *      go first.  The node that had such a slot loses it (remap = -1); weight becomes 1 and node the new node.
+ *      slots of least (weight, slot) among those not hit are given to the first m misses, in ascending order; free slots have
+ *      weight 0 and so go first.  The node that had such a slot loses it (remap = -1); weight becomes 1 and node the new node.
  *   3. slots[i] (device int32 [n_max]) = the slot of nodes[i], -1 where there was none left.
  *      fresh[j] (device int32 [n_max]) = the place in nodes of the j-th miss that got a slot, fresh_slots[j] its slot (ascending: what
  *      dci_kv_write wants); both -1 from j = m on, up to n_max.

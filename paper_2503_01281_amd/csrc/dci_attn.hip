@@ -3,22 +3,26 @@
 // For a row i and a head h, over the entries e of the row's list:  z_e = scale (q_i . K_e) + bias_e,  out = sum exp(z_e) V_e / sum exp(z_e).
 // One pass over the list: a running maximum m, the sum l of exp(z - m) and the accumulator of exp(z - m) V, the last two rescaled
 // when m grows.  Every K and V row that an entry names is read once, straight into registers, 16 columns of an 8-bit row to a lane, 8 of others:
-//   a head's columns lie in LH = 1 .. 32 adjacent lanes, in pieces of 16 bytes that follow each other from lane to lane, so that a load asks for 128
-//   bytes in one place wherever a head has them (a lane has one piece, of a 32-bit row two; the piece that a head ends in is its last 16 bytes, whichever of them the piece before has as well:
-//   those count once in a score, and are written twice alike), the heads of a row side by side, P lanes in all (a power of two up to 64; more
-//   heads are shared out between wavefronts).  A score is a sum over LH lanes, and the lanes of a head then hold what they need
-//   for their columns of the output: nothing passes through LDS.
+//   a head's columns lie in LH = 1 .. 32 adjacent lanes, in pieces of 16 bytes that follow each other from lane to lane, so that a load asks
+//   for 128 bytes in one place wherever a head has them (a lane has one piece, of a 32-bit row two; the piece that a head ends in is its last 16
+//   bytes, whichever of them the piece before has as well: those count once in a score, and are written twice alike), the heads of a row side by
+//   side, P lanes in all (a power of two up to 64; more heads are shared out between wavefronts).  A score is a sum over LH lanes, and the lanes of
+//   a head then hold what they need for their columns of the output: nothing passes through LDS.
 //   The 64 / P groups of lanes of a wavefront work on rows of their own, or R of them on one row, each on every R-th entry, and join their
 //   (m, l, acc) at the row's end.
 //   A group's lanes look up P entries at a time, an entry to a lane, the next P while these are worked on; what an entry names then goes from its
 //   lane to all of them.  An entry that is left out takes row 0's place and a score of -inf.
-//   Query heads that share a key head are worked on together, up to four of them (GQ), from the same registers.
-// Lists of more than 64 entries, and all where there is a handful of them, are worked on by chunks: a wavefront takes `chunk` entries of the whole array of entries, so that neither the
-// number nor the length of lists needs to be known, and finds the rows they belong to (a 64-way search in indptr).  A list that lies within a chunk
-// is done there; of others (m, l, acc) of the piece is left in the workspace, for k_attn_join to add up in order.  A chunk has at most two such
-// pieces: that of a list that goes on from before or begins with the chunk (0), and that of one that begins inside and goes on behind it (1).
-// What bounds it: the rows' bytes.  A row of the cache is 2 * kv_heads * head_dim bytes in one place, so a gather of whole rows
-// goes at nearly the rate of a copy.
+//   Query heads that share a key head are worked on together, up to four of them (GQ), from the same registers (24,576 rows of nine 32-bit entries,
+//   16 query heads of 64 on four: 105 us; two at a time 112).
+// Lists of more than 64 entries, and all where there is a handful of them, are worked on by chunks: a wavefront takes `chunk` entries of the whole
+// array of entries, so that neither the number nor the length of lists needs to be known, and finds the rows they belong to (a 64-way search in
+// indptr).  A list that lies within a chunk is done there; of others (m, l, acc) of the piece is left in the workspace, for k_attn_join to add up in
+// order.  A chunk has at most two such pieces: that of a list that goes on from before or begins with the chunk (0), and that of one that begins
+// inside and goes on behind it (1).
+// What bounds it: the rows that entries name, line by line.  98,304 rows of 12 entries of four 8-bit heads of 64, with weights: 140 us (129 without
+// them), 0.92 GB between L2 and memory by the counters, 6.5 TB/s.  Dense 32-bit rows, 24,576 by 9 entries of 2 KB: 71 us, 0.47 GB, 6.6 TB/s.
+// Where rows are few or entries narrow it is the chain of reads, bounds - source - slot - row: 10,007 rows of 20 entries of three heads of 41 with
+// biases and weights take 47 us at 2.7 TB/s.
 #include "dci_kv.h"
 
 namespace dci {
@@ -166,20 +170,6 @@ __device__ __forceinline__ int first_column(const Attn& a, const Place& pl, int 
 // A lane's columns of a row of the cache, whose heads are padded to whole pieces
 __device__ __forceinline__ int cached_column(const Attn& a, const Place& pl) {
   return pl.part * kChunk < a.dim ? pl.part * kChunk : 0;
-}
-
-// x[j] = x[j + by], 0 beyond the end (by < 16)
-template <int N>
-__device__ __forceinline__ void shift_down(float (&x)[N], int by) {
-#pragma unroll
-  for (int step = 8; step; step >>= 1) {
-    const bool go = by & step;
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-      const float far = j + step < N ? x[j + step < N ? j + step : j] : 0.f;
-      x[j] = go ? far : x[j];
-    }
-  }
 }
 
 // Entries [e0, e1) that are gone through: none where nothing can be named
@@ -632,8 +622,9 @@ __global__ __launch_bounds__(kAttnBlock, waves_per_simd(TYPE, GQ)) void k_attn_r
 //              (2^-27, 2^-18 of it are lost): part j / H of head j % H is row j, so the parts cost no instruction of their own.  The value's
 //              scale is P's.  A lane brings W / 16 bytes of eight entries' values, side by side over j, pairs two entries' bytes with v_perm
 //              and converts.
-// At the end the parts of O are added up through LDS.  It does a quarter of the vector instructions of k_attn_chunks for four heads to a group
-// (chunks of 640,000 entries, 8 key heads of 128, 32 query heads: 380 us there); what bounds it are the requests for rows.
+// At the end the parts of O are added up through LDS.  It does a quarter of the vector instructions of k_attn_chunks for four heads to a group:
+// 640,000 entries of eight key heads of 128 with 32 query heads take 281 to 297 us, 380 by k_attn_chunks.  What bounds it are the rows, 1.5 GB there
+// by the counters, 5 to 5.4 TB/s; a million entries of four heads of 64 take 117 us at 4.8 TB/s, with 80 requests to L2 a nanosecond.
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -903,7 +894,7 @@ __global__ __launch_bounds__(kAttnBlock, W == 64 ? 3 : 2) void k_attn_groups(con
 
 // One workgroup per row and head, or, where there are fewer of them, per chunk and head, for the long list that begins in the chunk and goes on behind
 // it: the list's pieces added up in order.  Their weights exp(m - max) are made 256 at a time, in LDS; columns lie side by side, in as many slices of
-// the pieces as the workgroup has room for.
+// the pieces as the workgroup has room for.  11 to 16 us behind long lists, a third of that the launch.
 __global__ __launch_bounds__(kAttnBlock) void k_attn_join(const Attn a, bool by_row) {
   const int head = (int)(blockIdx.x % (unsigned)a.heads);
   const long long n = rows_of(a);
@@ -1032,11 +1023,14 @@ Split split_of(const dci_attn& t, int type, bool accumulate) {
   s.p_log2 = log2_up((int64_t)s.wave_heads << s.lh_log2);
   if (s.p_log2 < 2) s.p_log2 = 2;  // entries are taken four at a time
   s.passes = (t.kv_heads + s.wave_heads - 1) / s.wave_heads * s.gq_passes;
-  // chunks of 64 to 512 entries: as long as there are wavefronts enough.  Shorter ones (16 or 32; a step of k_attn_groups is 32 entries) where that leaves
-  // only a few to a compute unit: 28,000 entries of seven 32-bit heads of 64 take 48 us in chunks of 32 and 55 in chunks of 64.  With more wavefronts
-  // the pieces cost more than they give: 37,000 entries of eight 16-bit heads of 128 on two take 46 us in chunks of 16, 38 in 32, 37 in 64.
+  // To k_attn_groups from three query heads to a key head on: 640,000 entries of eight key heads of 128 take 297 us there for three to a group and 385 in
+  // k_attn_chunks, 306 and 700 for eight; for two 294 and 261 (a million entries of four of 64: 132 and 169, 146 and 289; 127 and 114).
   s.matrix = type == kE4M3 && group >= 3 && !t.bias && (t.head_dim == 64 || t.head_dim == 128 || t.head_dim == 256);
   const int64_t waves = s.matrix ? (int64_t)t.kv_heads * ((group + 7) / 8) : ((int64_t)t.kv_heads * kv_width(t.head_dim) + 1023) / 1024 * ((group + gq - 1) / gq);
+  // Chunks of 64 to 512 entries: as long as there are wavefronts enough (with half as many 640,000 entries of eight heads of 128, two query heads to
+  // each, take 309 us for 261).  Shorter ones (16 or 32; a step of k_attn_groups is 32 entries) where that leaves only a few to a compute unit: 28,000
+  // entries of seven 32-bit heads of 64 take 48 us in chunks of 32 and 55 in chunks of 64.  With more wavefronts the pieces cost more than they give:
+  // 37,000 entries of eight 16-bit heads of 128 on two take 46 us in chunks of 16, 38 in 32, 37 in 64.
   s.chunk = s.matrix ? 32 : 16;
   while (s.chunk < 512 && t.n_edges / s.chunk * waves > (s.chunk < 64 ? kFewWaves : kWantedWaves)) s.chunk *= 2;
   const int64_t longest = t.max_list > 0 && t.max_list < t.n_edges ? t.max_list : t.n_edges;
@@ -1166,7 +1160,7 @@ int32_t attn(dci_ctx* ctx, const dci_attn& t, int type, Attn a, bool accumulate)
   const bool all_by_chunks = by_row && t.n_rows <= 16;
   a.short_list = all_by_chunks ? 0 : kShort;
   // lane groups to a row: one, unless that leaves wavefronts to be had (no more then than there are entries in a list) or, with weights, the scores
-  // of the longest list would not all be at hand at its end
+  // of the longest list would not all be at hand at its end.  (12,000 rows of 12 entries of four heads of 64: 23 us, 27 with two groups to a row.)
   const int groups_log2 = 6 - s.p_log2;
   const int64_t mean = t.n_edges / t.n_rows, longest = s.n_chunks ? kShort : t.max_list > 0 ? t.max_list : t.n_edges;
   a.r_log2 = 0;

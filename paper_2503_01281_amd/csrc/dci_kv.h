@@ -17,11 +17,6 @@ inline int log2_up(int64_t x) {
 inline int kv_width(int head_dim) { return (head_dim + kChunk - 1) / kChunk * kChunk; }
 constexpr int type_bytes(int type) { return type == kE4M3 ? 1 : type == DCI_F32 ? 4 : 2; }
 inline bool known_type(int32_t type) { return type == DCI_F32 || type == DCI_BF16 || type == DCI_F16; }
-// Whether rows can be read and written 16 bytes at a time: every head starts on 16 bytes, and none ends inside 16.
-inline bool by_16_bytes(const void* base, int64_t stride, int head_dim, int type) {
-  const int64_t b = type_bytes(type);
-  return reinterpret_cast<uintptr_t>(base) % 16 == 0 && stride * b % 16 == 0 && head_dim * b % 16 == 0;
-}
 inline bool aligned_rows(const void* base, int type) { return reinterpret_cast<uintptr_t>(base) % (unsigned)type_bytes(type) == 0; }
 
 // The current device is the context's while this lives, whatever it was before.
@@ -45,6 +40,8 @@ int32_t check_kv_cache(dci_ctx* ctx, const dci_kv_cache* cache);
 
 // Sixteen bytes anywhere: the loads and stores of rows need no alignment beyond their type's.
 typedef unsigned u32x4_any __attribute__((ext_vector_type(4), aligned(1)));
+typedef unsigned u32x2_any __attribute__((ext_vector_type(2), aligned(1)));
+typedef unsigned u32_any __attribute__((aligned(1)));
 __device__ __forceinline__ uint4 load_16(const char* p) {
   const u32x4_any v = *reinterpret_cast<const u32x4_any*>(p);
   return make_uint4(v.x, v.y, v.z, v.w);
@@ -68,7 +65,7 @@ struct Chunk {
 #pragma unroll
     for (int j = 0; j < kWords; ++j) w[j] = load_16(p + 16 * j);
   }
-  // The first `cols` (1 .. COLS) of them from p, the others 0; wide: by 16 bytes (by_16_bytes), else number by number.
+  // The first `cols` (1 .. COLS) of them from p, the others 0; wide: by 16 bytes (cols are a multiple of them), else number by number.
   __device__ __forceinline__ void load(const char* p, int cols, bool wide) {
     if (TYPE == kE4M3) {
       w[0] = *reinterpret_cast<const uint4*>(p);
@@ -116,6 +113,20 @@ struct Chunk {
     }
   }
 };
+
+// x[j] = x[j + by], 0 beyond the end (by < 16)
+template <int N>
+__device__ __forceinline__ void shift_down(float (&x)[N], int by) {
+#pragma unroll
+  for (int step = 8; step; step >>= 1) {
+    const bool go = by & step;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const float far = j + step < N ? x[j + step < N ? j + step : j] : 0.f;
+      x[j] = go ? far : x[j];
+    }
+  }
+}
 
 // 16 columns from p as numbers
 template <int TYPE, int COLS>

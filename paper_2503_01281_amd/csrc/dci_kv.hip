@@ -45,7 +45,7 @@ struct KvWrite {
   int type;
   const char* from[2];  // keys, values
   long long stride[2];  // bytes
-  bool wide[2];
+  bool wide, odd;       // heads of 16 columns at least, or of a multiple of 16 bytes: read by 16 bytes; of those, heads that end inside 16 bytes
   unsigned char* codes;
   float* scales;
   long long n_slots;
@@ -97,14 +97,27 @@ __device__ __forceinline__ float peak_of(const float (&x)[kChunk]) {
   return amax;
 }
 
+// A lane's 16 columns of a head, from `col` on.  Where the head ends inside 16 bytes of them (odd), its last 16 columns are read, wherever they
+// lie: `skip` of those are the lane's before, and shift_down brings its own to their place, zeros behind them.  (Number by number, 200,000 rows of
+// 16-bit heads of 97 take twice as long; heads of 72 take 8 % less as they are than with a shift.)
+struct Piece {
+  int from, cols, skip;
+  __device__ __forceinline__ Piece(int col, int dim, bool odd) {
+    from = odd ? min(col, dim - kChunk) : col;
+    cols = col >= dim ? 0 : odd ? kChunk : min(kChunk, dim - col);
+    skip = cols ? col - from : 0;
+  }
+};
+
 // The block whose entries are rows [i, i + rows) of the list, for one head and kind, by a whole wavefront: first the maximum of what is to be
 // written, then the scale, the block's other rows where that grew, the rows.  mine: lane t's slot, -1 where it is none of the block's.
 template <int TYPE>
 __device__ void write_block(const KvWrite& a, int kind, int head, long long i, int mine) {
   const int lane = lane_id(), lh = 1 << a.lh_log2, at_once = kWave >> a.lh_log2;
-  const int r = lane >> a.lh_log2, col = (lane & (lh - 1)) * kChunk, cols = min(kChunk, max(0, a.dim - col));
+  const int r = lane >> a.lh_log2, col = (lane & (lh - 1)) * kChunk;
+  const Piece piece(col, a.dim, a.odd);
   const int width = (a.dim + kChunk - 1) / kChunk * kChunk, block_slots = 1 << a.block_log2;
-  const char* from = a.from[kind] + ((long long)head * a.dim + col) * type_bytes(TYPE);
+  const char* from = a.from[kind] + ((long long)head * a.dim + piece.from) * type_bytes(TYPE);
   unsigned char* to = a.codes + (long long)(kind * a.kv_heads + head) * width + col;
   const long long row_bytes = 2ll * a.kv_heads * width;
   const unsigned long long with = __ballot(mine >= 0);
@@ -115,8 +128,8 @@ __device__ void write_block(const KvWrite& a, int kind, int head, long long i, i
   float amax = 0.f, x[kChunk];
   for (int t0 = 0; t0 < rows; t0 += at_once) {
     const int t = t0 + r;
-    if (t < rows && cols > 0) {
-      read_chunk_as<TYPE>(from + (i + t) * a.stride[kind], cols, a.wide[kind], x);
+    if (t < rows && piece.cols > 0) {
+      read_chunk_as<TYPE>(from + (i + t) * a.stride[kind], piece.cols, a.wide, x);
       amax = fmaxf(amax, peak_of(x));
     }
   }
@@ -154,7 +167,8 @@ __device__ void write_block(const KvWrite& a, int kind, int head, long long i, i
     if (t < rows && col < width) {
 #pragma unroll
       for (int j = 0; j < kChunk; ++j) x[j] = 0.f;
-      if (cols > 0) read_chunk_as<TYPE>(from + (i + t) * a.stride[kind], cols, a.wide[kind], x);
+      if (piece.cols > 0) read_chunk_as<TYPE>(from + (i + t) * a.stride[kind], piece.cols, a.wide, x);
+      if (a.odd) shift_down(x, piece.skip);
       *reinterpret_cast<uint4*>(to + (long long)s * row_bytes) = encode(x, e);
     }
   }
@@ -165,7 +179,8 @@ __device__ void write_block(const KvWrite& a, int kind, int head, long long i, i
 // entry is among its own, whole; the list ascends, so a block's entries are together, and no other wavefront touches this head of the block.  Where
 // a row lies does not depend on its slot, so the rows, keys and values, are on their way while the slots are looked at.  The blocks that end among
 // the wavefront's entries are done side by side, their maxima joined in LDS; one that goes on behind them, and one whose other rows have to be rounded
-// anew, is done on its own (write_block).  What bounds it: the rows' bytes, read and written once.
+// anew, is done on its own (write_block).  What bounds it: the rows' bytes, read and written once (half a million rows of 512 numbers in 16 bits:
+// 180 us, 0.78 GB, 4.3 TB/s).
 template <int TYPE, int T>
 __global__ __launch_bounds__(kKvBlock) void k_kv_write(const KvWrite a) {
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
@@ -176,17 +191,18 @@ __global__ __launch_bounds__(kKvBlock) void k_kv_write(const KvWrite a) {
   const long long n = a.n_dev ? min(a.n_max, max(0ll, *a.n_dev)) : a.n_max;
   __shared__ unsigned peaks[kKvWaves][2][kWave];
   if (i0 >= n) return;
-  const int r = lane >> a.lh_log2, col = (lane & (lh - 1)) * kChunk, cols = min(kChunk, max(0, a.dim - col));
+  const int r = lane >> a.lh_log2, col = (lane & (lh - 1)) * kChunk;
+  const Piece piece(col, a.dim, a.odd);
   const int width = (a.dim + kChunk - 1) / kChunk * kChunk;
   Chunk<TYPE> x[2][T];
 #pragma unroll
   for (int kind = 0; kind < 2; ++kind) {
-    const char* from = a.from[kind] + ((long long)head * a.dim + col) * type_bytes(TYPE);
+    const char* from = a.from[kind] + ((long long)head * a.dim + piece.from) * type_bytes(TYPE);
 #pragma unroll
     for (int k = 0; k < T; ++k) {
       x[kind][k].clear();
       const long long i = i0 + k * at_once + r;
-      if (i < n && cols > 0) x[kind][k].load(from + i * a.stride[kind], cols, a.wide[kind]);
+      if (i < n && piece.cols > 0) x[kind][k].load(from + i * a.stride[kind], piece.cols, a.wide);
     }
   }
   auto slot_at = [&](long long i) {
@@ -263,6 +279,7 @@ __global__ __launch_bounds__(kKvBlock) void k_kv_write(const KvWrite a) {
         float y[kChunk];
 #pragma unroll
         for (int j = 0; j < kChunk / 2; ++j) x[kind][k].pair(j, y[2 * j], y[2 * j + 1]);
+        if (a.odd) shift_down(y, piece.skip);
         *reinterpret_cast<uint4*>(a.codes + ((2ll * to_s + kind) * a.kv_heads + head) * width + col) = encode(y, to_e);
       }
     }
@@ -291,19 +308,20 @@ struct KvRead {
   int lanes_log2;  // lanes to a row
 };
 
-// 16 bytes of the output to a lane where that goes (4 or 8 columns), else a number.  Lanes lie side by side along a row, `lanes` of them (a
+// 16 bytes of the output to a lane (4 or 8 columns; a head's last piece ends with it, and has columns of the one before as well), a number where heads
+// are narrower.  Lanes lie side by side along a row, `lanes` of them (a
 // power of two up to a workgroup) to a row, and a lane keeps its place in the rows; four rows at a time.  What bounds it: the bytes
-// written.
+// written (half a million rows of 512 numbers as fp32: 252 us, 1.3 GB, 5.2 TB/s).
 template <int TYPE, bool WIDE>
 __global__ __launch_bounds__(kKvBlock) void k_kv_read(const KvRead a) {
   constexpr int kPer = WIDE ? 16 / type_bytes(TYPE) : 1, kAtOnce = 4;
   const int width = (a.dim + kChunk - 1) / kChunk * kChunk;
-  const unsigned head_pieces = (unsigned)a.dim / kPer, row_pieces = 2u * a.kv_heads * head_pieces;
+  const unsigned head_pieces = (unsigned)(a.dim + kPer - 1) / kPer, row_pieces = 2u * a.kv_heads * head_pieces;
   const long long n = a.n_dev ? min(a.n_max, max(0ll, *a.n_dev)) : a.n_max;
   const int lanes = 1 << a.lanes_log2, rows = kKvBlock >> a.lanes_log2;
   const long long step = (long long)gridDim.x * rows;
   for (unsigned in = threadIdx.x & (lanes - 1); in < row_pieces; in += lanes) {
-    const unsigned part = in / head_pieces, col = (in - part * head_pieces) * kPer;
+    const unsigned part = in / head_pieces, col = min((in - part * head_pieces) * kPer, (unsigned)(a.dim - kPer));
     const unsigned kind = part / (unsigned)a.kv_heads, head = part - kind * a.kv_heads;
     const unsigned char* codes = a.codes + (long long)part * width + col;
     const float* scales = a.scales + 2 * head + kind;
@@ -325,9 +343,9 @@ __global__ __launch_bounds__(kKvBlock) void k_kv_read(const KvRead a) {
         if (s[k] >= 0) {
           const unsigned char* p = codes + s[k] * (2ll * a.kv_heads * width);
           if (!WIDE) c[k].w[0].x = *p;
-          else if (kPer == 4) c[k].w[0].x = *reinterpret_cast<const unsigned*>(p);
+          else if (kPer == 4) c[k].w[0].x = *reinterpret_cast<const u32_any*>(p);
           else {
-            const uint2 u = *reinterpret_cast<const uint2*>(p);
+            const u32x2_any u = *reinterpret_cast<const u32x2_any*>(p);
             c[k].w[0].x = u.x;
             c[k].w[0].y = u.y;
           }
@@ -349,9 +367,9 @@ __global__ __launch_bounds__(kKvBlock) void k_kv_read(const KvRead a) {
           if (TYPE == DCI_F32) *reinterpret_cast<float*>(o) = y[0];
           else *reinterpret_cast<unsigned short*>(o) = (unsigned short)two<TYPE>(y[0], 0.f);
         } else if (TYPE == DCI_F32) {
-          *reinterpret_cast<float4*>(o) = make_float4(y[0], y[1], y[2], y[3]);
+          store_16(o, make_uint4(__float_as_uint(y[0]), __float_as_uint(y[1]), __float_as_uint(y[2]), __float_as_uint(y[3])));
         } else {
-          *reinterpret_cast<uint4*>(o) = make_uint4(two<TYPE>(y[0], y[1]), two<TYPE>(y[2], y[3]), two<TYPE>(y[4], y[5]), two<TYPE>(y[6], y[7]));
+          store_16(o, make_uint4(two<TYPE>(y[0], y[1]), two<TYPE>(y[2], y[3]), two<TYPE>(y[4], y[5]), two<TYPE>(y[6], y[7])));
         }
       }
     }
@@ -362,7 +380,8 @@ template <int TYPE>
 void launch_write(int tiles, const KvWrite& a, unsigned grid, hipStream_t stream) {
   if (tiles == 1) hipLaunchKernelGGL((k_kv_write<TYPE, 1>), dim3(grid), dim3(kKvBlock), 0, stream, a);
   else if (tiles == 2) hipLaunchKernelGGL((k_kv_write<TYPE, 2>), dim3(grid), dim3(kKvBlock), 0, stream, a);
-  else hipLaunchKernelGGL((k_kv_write<TYPE, 4>), dim3(grid), dim3(kKvBlock), 0, stream, a);
+  else if (tiles == 4) hipLaunchKernelGGL((k_kv_write<TYPE, 4>), dim3(grid), dim3(kKvBlock), 0, stream, a);
+  else hipLaunchKernelGGL((k_kv_write<TYPE, 8>), dim3(grid), dim3(kKvBlock), 0, stream, a);
 }
 template <int TYPE>
 void launch_read(bool wide, const KvRead& a, unsigned grid, hipStream_t stream) {
@@ -392,11 +411,13 @@ int32_t check_rows(dci_ctx* ctx, const dci_kv_cache* cache, const int32_t* slots
 // digit of their highest bits would be the same for all), then digits of 13 bits of the rest, until the slots at the border are all alike or
 // all wanted.  A digit's counts are added up by workgroup in LDS, then in memory; every workgroup of the next kernel looks for the border in them.  Three
 // digits tell weights apart that differ by 2^-33 of themselves (all of them below 16); what is left after that, one workgroup does by itself.
-// Slots and misses are kept as bit masks, numbered by prefix sums over tiles of them, and the j-th slot goes to the j-th miss.  While the call runs, the
-// slots that are hit have the highest bit of their weight set.
+// Slots and misses are kept as bit masks, numbered by prefix sums over tiles of them, and the j-th slot goes to the j-th miss.  While the call
+// runs, the slots that are hit have the highest bit of their weight set.
 // Nothing waits for another workgroup: what a kernel leaves is looked through by every workgroup of the next (the counts of a digit, the sums of at
-// most 1,024 tiles).  What bounds it: seven launches (eight for large caches) one after the other, each a few dependent reads long, and 8 bytes per slot and digit that
-// mostly come from the last-level cache.
+// most 1,024 tiles).  What bounds it: seven launches (eight for large caches) one after the other, each a few dependent reads long, and for large
+// batches the random lines of remap, weights and nodes.  400,000 nodes on a million slots take 89 us: 23 of them the look-up (0.55 million lines that
+// L2 does not have, 24 a nanosecond, and as many atomics), 11 the first digit, 12 the other two, 10 numbering, 15 giving, 8 the slots; 3,000 nodes
+// on 65,536 slots take 37 us in launches of 3 to 7 us.
 
 constexpr int kDigit = 13, kBins = 1 << kDigit, kDigits = 3;
 constexpr int kMantissa = 7;  // of the first digit
@@ -843,8 +864,8 @@ int32_t dci_kv_write(dci_ctx* ctx, const dci_kv_cache* cache, const int32_t* slo
   a.from[1] = static_cast<const char*>(v);
   a.stride[0] = k_stride * bytes;
   a.stride[1] = v_stride * bytes;
-  a.wide[0] = dci::by_16_bytes(k, k_stride, cache->head_dim, dtype);
-  a.wide[1] = dci::by_16_bytes(v, v_stride, cache->head_dim, dtype);
+  a.wide = cache->head_dim >= dci::kChunk || cache->head_dim * bytes % 16 == 0;
+  a.odd = a.wide && cache->head_dim * bytes % 16 != 0;
   a.codes = cache->codes;
   a.scales = cache->scales;
   a.n_slots = cache->n_slots;
@@ -853,10 +874,12 @@ int32_t dci_kv_write(dci_ctx* ctx, const dci_kv_cache* cache, const int32_t* slo
   a.dim = cache->head_dim;
   a.lh_log2 = dci::log2_up((cache->head_dim + dci::kChunk - 1) / dci::kChunk);
   a.host_flag = ctx->host_flag;
-  // entries to a wavefront: a block's, as far as four times the rows that it has lanes for go
-  const int at_once = dci::kWave >> a.lh_log2;
+  // Entries to a wavefront: a block's, as far as four times the rows that it has lanes for go, eight times where many blocks may be written whole (a
+  // block that does not fit is read twice).  Heads of 128, blocks of 64, 16-bit rows: 200,000 of 200,000 slots 469 us with eight and 611 with four,
+  // 20,000 of them 270 and 256.
+  const int at_once = dci::kWave >> a.lh_log2, most = n_max >= cache->n_slots / 2 ? 8 : 4;
   int tiles = 1;
-  while (tiles < 4 && tiles * at_once < cache->block) tiles *= 2;
+  while (tiles < most && tiles * at_once < cache->block) tiles *= 2;
   const int64_t waves = (n_max + tiles * at_once - 1) / (tiles * at_once) * cache->kv_heads;
   const int64_t grid = (waves + dci::kKvWaves - 1) / dci::kKvWaves;
   if (waves > 0x7FFFFFFFll) return dci::fail(ctx, DCI_ERR_UNSUPPORTED, "key/value rows: too many rows and heads for one call");
@@ -885,14 +908,14 @@ int32_t dci_kv_read(dci_ctx* ctx, const dci_kv_cache* cache, const int32_t* slot
   a.to[1] = static_cast<char*>(v);
   a.stride[0] = k_stride * bytes;
   a.stride[1] = v_stride * bytes;
-  const bool wide = dci::by_16_bytes(k, k_stride, cache->head_dim, dtype) && dci::by_16_bytes(v, v_stride, cache->head_dim, dtype);
+  const bool wide = cache->head_dim * bytes >= 16;
   a.codes = cache->codes;
   a.scales = cache->scales;
   a.n_slots = cache->n_slots;
   a.block_log2 = dci::log2_up(cache->block);
   a.kv_heads = cache->kv_heads;
   a.dim = cache->head_dim;
-  const int64_t pieces = 2ll * cache->kv_heads * (wide ? cache->head_dim * bytes / 16 : cache->head_dim);
+  const int64_t pieces = 2ll * cache->kv_heads * (wide ? (cache->head_dim * bytes + 15) / 16 : cache->head_dim);
   a.lanes_log2 = dci::log2_up(pieces);
   if (a.lanes_log2 > 8) a.lanes_log2 = 8;  // a workgroup
   const int64_t rows = dci::kKvBlock >> a.lanes_log2;
