@@ -599,7 +599,8 @@ def dci_attn_cached(ctx: Context, q: torch.Tensor, cache: KvCache, indptr: torch
     need = ctx.lib.dci_attn_workspace_bytes(C.byref(a), int(accumulate))
     if need:
         ctx.ensure_workspace(need)
-    ctx.check(ctx.lib.dci_attn_cached(ctx.handle, C.byref(a), C.byref(cache.c), _ptr(slots), int(accumulate)))
+    at = _ptr(slots) if slots is None or slots.numel() else _ptr(indptr)  # without sources: read by nobody, but not null, which has a meaning
+    ctx.check(ctx.lib.dci_attn_cached(ctx.handle, C.byref(a), C.byref(cache.c), at, int(accumulate)))
 
 
 def _kv_rows(cache, slots, k, v):

@@ -1080,7 +1080,7 @@ int32_t check_attn(dci_ctx* ctx, const dci_attn* t) {
                 (long long)t->q_stride, (long long)t->out_stride);
   if (!aligned_rows(t->q, t->dtype) || !aligned_rows(t->out, t->dtype))
     return fail(ctx, DCI_ERR_INVALID_ARG, "attention: q and out must be aligned to their type");
-  if (t->bias ? t->bias_heads != 1 && t->bias_heads != t->n_heads : t->bias_heads != 0)
+  if (t->bias ? t->bias_heads != 1 && t->bias_heads != t->n_heads : t->bias_heads != 0 && t->n_edges > 0)  // (an array of nothing may be null)
     return fail(ctx, DCI_ERR_INVALID_ARG, "attention: bias_heads is 1 or n_heads with a bias and 0 without, not %d", t->bias_heads);
   return DCI_OK;
 }

@@ -214,6 +214,32 @@ def test_rows_behind_the_count_are_left_alone():
             check(out, lse, [w[:rows] for w in want[:2]] + [None] + [w[:rows] for w in want[3:5]], rows, "fp32")
 
 
+@pytest.mark.parametrize("rows,edges,sources", [(3, 0, 5), (3, 0, 0), (3, 9, 0), (3, 700, 0), (0, 0, 5), (0, 0, 0)])
+@pytest.mark.parametrize("bias_heads", [0, 1, 4])
+def test_calls_with_nothing_to_attend_to(rows, edges, sources, bias_heads):
+    """No rows, no entries, no sources: tensors without elements, whose addresses are null, are taken as what they are."""
+    import paper_2503_01281_amd as dci
+    ctx = dci.Context(0)
+    heads, dim = 4, 64
+    cache, _ = make_cache(dci, 50, heads, dim, 16, np.random.default_rng(1))
+    before = cache.weight.clone()
+    indptr = torch.linspace(0, edges, rows + 1).long().cuda() if rows else torch.zeros(1, dtype=torch.int64, device="cuda")
+    src = (torch.arange(edges, dtype=torch.int32) % 50).cuda()
+    bias = torch.zeros(edges, bias_heads, device="cuda") if bias_heads else None
+    q = torch.randn(rows, heads, dim, device="cuda")
+    kv = torch.randn(sources, heads, dim, device="cuda")
+    slots = torch.arange(sources, dtype=torch.int32, device="cuda")
+    for cached in (False, True):
+        for max_list in (0, 64):
+            out, lse = torch.full_like(q, 7.0), torch.full((rows, heads), 7.0, device="cuda")
+            if cached:
+                dci.dci_attn_cached(ctx, q, cache, indptr, src, out, 0.125, slots=slots, lse=lse, bias=bias, accumulate=True, max_list=max_list)
+            else:
+                dci.dci_attn_forward(ctx, q, kv, kv, indptr, src, out, 0.125, lse=lse, bias=bias, max_list=max_list)
+            ctx.sync()
+            assert (out == 0).all() and torch.isneginf(lse).all() and torch.equal(cache.weight, before)
+
+
 @pytest.mark.parametrize("length", [10, 500])
 @pytest.mark.parametrize("cached", [False, True])
 def test_left_out_entries_may_hold_anything(length, cached):
