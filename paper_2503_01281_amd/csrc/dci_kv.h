@@ -50,6 +50,11 @@ __device__ __forceinline__ void store_16(char* p, uint4 v) {
   const u32x4_any u = {v.x, v.y, v.z, v.w};
   *reinterpret_cast<u32x4_any*>(p) = u;
 }
+// Past the caches
+__device__ __forceinline__ void store_16_past(char* p, uint4 v) {
+  const u32x4_any u = {v.x, v.y, v.z, v.w};
+  __builtin_nontemporal_store(u, reinterpret_cast<u32x4_any*>(p));
+}
 
 // COLS columns of a row as they lie in memory.
 template <int TYPE, int COLS = kChunk>

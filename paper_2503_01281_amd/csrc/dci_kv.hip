@@ -68,17 +68,18 @@ __device__ __forceinline__ float exp2_of(int e) { return __uint_as_float((unsign
 // numbers beyond 464 as well, and those only kMaxExp leaves.)
 __device__ __forceinline__ uint4 encode(const float (&x)[kChunk], int e) {
   const float f = exp2_of(-e);
+  float y[kChunk];
+#pragma unroll
+  for (int j = 0; j < kChunk; ++j) y[j] = x[j] * f;
+  if (__builtin_expect(e == kMaxExp, 0)) {
+#pragma unroll
+    for (int j = 0; j < kChunk; ++j) y[j] = is_number(y[j]) ? fminf(fmaxf(y[j], -448.f), 448.f) : y[j];
+  }
   unsigned w[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    float y[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      y[k] = x[4 * j + k] * f;
-      if (e == kMaxExp && is_number(y[k])) y[k] = fminf(fmaxf(y[k], -448.f), 448.f);
-    }
-    int u = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
-    u = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], u, true);
+    int u = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * j], y[4 * j + 1], 0, false);
+    u = __builtin_amdgcn_cvt_pk_fp8_f32(y[4 * j + 2], y[4 * j + 3], u, true);
     w[j] = (unsigned)u;
   }
   return make_uint4(w[0], w[1], w[2], w[3]);
@@ -180,7 +181,7 @@ __device__ void write_block(const KvWrite& a, int kind, int head, long long i, i
 // a row lies does not depend on its slot, so the rows, keys and values, are on their way while the slots are looked at.  The blocks that end among
 // the wavefront's entries are done side by side, their maxima joined in LDS; one that goes on behind them, and one whose other rows have to be rounded
 // anew, is done on its own (write_block).  What bounds it: the rows' bytes, read and written once (half a million rows of 512 numbers in 16 bits:
-// 180 us, 0.78 GB, 4.3 TB/s).
+// 149 to 176 us, by what the last-level cache has of them, 0.78 GB, 4.4 to 5.2 TB/s).
 template <int TYPE, int T>
 __global__ __launch_bounds__(kKvBlock) void k_kv_write(const KvWrite a) {
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
@@ -311,8 +312,8 @@ struct KvRead {
 // 16 bytes of the output to a lane (4 or 8 columns; a head's last piece ends with it, and has columns of the one before as well), a number where heads
 // are narrower.  Lanes lie side by side along a row, `lanes` of them (a
 // power of two up to a workgroup) to a row, and a lane keeps its place in the rows; four rows at a time.  What bounds it: the bytes
-// written (half a million rows of 512 numbers as fp32: 252 us, 1.3 GB, 5.2 TB/s).
-template <int TYPE, bool WIDE>
+// written (PAST: past the caches; half a million rows of 512 numbers as fp32: 268 us, 1.3 GB, 4.9 TB/s).
+template <int TYPE, bool WIDE, bool PAST>
 __global__ __launch_bounds__(kKvBlock) void k_kv_read(const KvRead a) {
   constexpr int kPer = WIDE ? 16 / type_bytes(TYPE) : 1, kAtOnce = 4;
   const int width = (a.dim + kChunk - 1) / kChunk * kChunk;
@@ -366,10 +367,11 @@ __global__ __launch_bounds__(kKvBlock) void k_kv_read(const KvRead a) {
         if (!WIDE) {
           if (TYPE == DCI_F32) *reinterpret_cast<float*>(o) = y[0];
           else *reinterpret_cast<unsigned short*>(o) = (unsigned short)two<TYPE>(y[0], 0.f);
-        } else if (TYPE == DCI_F32) {
-          store_16(o, make_uint4(__float_as_uint(y[0]), __float_as_uint(y[1]), __float_as_uint(y[2]), __float_as_uint(y[3])));
         } else {
-          store_16(o, make_uint4(two<TYPE>(y[0], y[1]), two<TYPE>(y[2], y[3]), two<TYPE>(y[4], y[5]), two<TYPE>(y[6], y[7])));
+          const uint4 u = TYPE == DCI_F32 ? make_uint4(__float_as_uint(y[0]), __float_as_uint(y[1]), __float_as_uint(y[2]), __float_as_uint(y[3]))
+                                          : make_uint4(two<TYPE>(y[0], y[1]), two<TYPE>(y[2], y[3]), two<TYPE>(y[4], y[5]), two<TYPE>(y[6], y[7]));
+          if (PAST) store_16_past(o, u);
+          else store_16(o, u);
         }
       }
     }
@@ -384,9 +386,10 @@ void launch_write(int tiles, const KvWrite& a, unsigned grid, hipStream_t stream
   else hipLaunchKernelGGL((k_kv_write<TYPE, 8>), dim3(grid), dim3(kKvBlock), 0, stream, a);
 }
 template <int TYPE>
-void launch_read(bool wide, const KvRead& a, unsigned grid, hipStream_t stream) {
-  if (wide) hipLaunchKernelGGL((k_kv_read<TYPE, true>), dim3(grid), dim3(kKvBlock), 0, stream, a);
-  else hipLaunchKernelGGL((k_kv_read<TYPE, false>), dim3(grid), dim3(kKvBlock), 0, stream, a);
+void launch_read(bool wide, bool past, const KvRead& a, unsigned grid, hipStream_t stream) {
+  if (!wide) hipLaunchKernelGGL((k_kv_read<TYPE, false, false>), dim3(grid), dim3(kKvBlock), 0, stream, a);
+  else if (past) hipLaunchKernelGGL((k_kv_read<TYPE, true, true>), dim3(grid), dim3(kKvBlock), 0, stream, a);
+  else hipLaunchKernelGGL((k_kv_read<TYPE, true, false>), dim3(grid), dim3(kKvBlock), 0, stream, a);
 }
 
 int32_t check_rows(dci_ctx* ctx, const dci_kv_cache* cache, const int32_t* slots, int64_t n_max, int32_t dtype, const void* k, int64_t k_stride,
@@ -918,13 +921,16 @@ int32_t dci_kv_read(dci_ctx* ctx, const dci_kv_cache* cache, const int32_t* slot
   const int64_t pieces = 2ll * cache->kv_heads * (wide ? (cache->head_dim * bytes + 15) / 16 : cache->head_dim);
   a.lanes_log2 = dci::log2_up(pieces);
   if (a.lanes_log2 > 8) a.lanes_log2 = 8;  // a workgroup
+  // An output of more than the last-level cache holds (256 MB) is not there when it is read next, and only drives out what is.  Past it 184,000 rows of
+  // 2 KB take 74 us for 98; half a million 268 for 254, but the write of their rows 149 for 181.  Below, 10,000 rows and attention over them take 43 for 41.
+  const bool past = n_max * pieces * 16 > 256ll << 20;
   const int64_t rows = dci::kKvBlock >> a.lanes_log2;
   int64_t grid = (n_max + rows * 4 - 1) / (rows * 4);
   if (grid > (int64_t)ctx->num_cus * 32) grid = (int64_t)ctx->num_cus * 32;
   dci::Timed timed(ctx, DCI_K_KV);
-  if (dtype == DCI_F32) dci::launch_read<DCI_F32>(wide, a, (unsigned)grid, ctx->stream);
-  else if (dtype == DCI_BF16) dci::launch_read<DCI_BF16>(wide, a, (unsigned)grid, ctx->stream);
-  else dci::launch_read<DCI_F16>(wide, a, (unsigned)grid, ctx->stream);
+  if (dtype == DCI_F32) dci::launch_read<DCI_F32>(wide, past, a, (unsigned)grid, ctx->stream);
+  else if (dtype == DCI_BF16) dci::launch_read<DCI_BF16>(wide, past, a, (unsigned)grid, ctx->stream);
+  else dci::launch_read<DCI_F16>(wide, past, a, (unsigned)grid, ctx->stream);
   DCI_LAUNCH_CHECK(ctx);
   return DCI_OK;
 }

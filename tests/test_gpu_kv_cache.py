@@ -275,6 +275,30 @@ def test_large_caches_and_batches():
         assert np.array_equal(g, w)
 
 
+@pytest.mark.parametrize("dim,dtype", [(64, "fp32"), (64, "bf16"), (41, "fp16"), (41, "fp32")])
+def test_a_read_of_more_than_the_last_level_cache(dim, dtype):
+    """One large read gives, to the bit, what reads of a few rows give; entries outside the cache leave their rows alone."""
+    import paper_2503_01281_amd as dci
+    ctx = dci.Context(0)
+    heads, n_slots, bytes_ = 4, 1000, 4 if dtype == "fp32" else 2
+    n = (300 << 20) // (2 * heads * dim * bytes_)
+    rng = np.random.default_rng(dim)
+    cache = dci.KvCache(ctx, n_slots, heads, dim, 16)
+    dci.dci_kv_write(ctx, cache, dev(np.arange(n_slots, dtype=np.int32)), some_rows(rng, n_slots, heads, dim, dtype).cuda(),
+                     some_rows(rng, n_slots, heads, dim, dtype).cuda())
+    one = [torch.empty(n_slots, heads, dim, dtype=TYPES[dtype], device="cuda") for _ in range(2)]
+    dci.dci_kv_read(ctx, cache, dev(np.arange(n_slots, dtype=np.int32)), *one)
+    at = torch.from_numpy(rng.integers(-5, n_slots + 5, n).astype(np.int32)).cuda()
+    got = [torch.full((n, heads * dim + 1), 7.0, dtype=TYPES[dtype], device="cuda")[:, :heads * dim].unflatten(1, (heads, dim)) for _ in range(2)]
+    dci.dci_kv_read(ctx, cache, at, *got)
+    ctx.sync()
+    inside = (at >= 0) & (at < n_slots)
+    whole = torch.int32 if bytes_ == 4 else torch.int16
+    for g, o in zip(got, one):
+        want = torch.where(inside[:, None, None], o[at.long().clamp(0, n_slots - 1)], torch.full((), 7.0, dtype=o.dtype, device="cuda"))
+        assert torch.equal(g.contiguous().view(whole), want.view(whole))
+
+
 def test_a_cache_beyond_4_gib():
     """Codes behind the 32-bit range of offsets: written, read and attended to."""
     import paper_2503_01281_amd as dci
