@@ -38,7 +38,7 @@ def test_workspace_sizes(lib):
 
     up = lambda x: -(-x // 256) * 256
     assert need() == need(1) == 0                          # short lists need none
-    chunks = -(-1500 // 64)
+    chunks = -(-1500 // 16)  # few entries: the shortest chunks
     parts = up(chunks * 2 * 4 * 2 * 4) + up(chunks * 2 * 4 * 64 * 4)
     assert need(max_list=0) == need(max_list=65) == parts  # lists that may be longer than 64
     assert need(1, max_list=0) == parts + up(1500 * 4 * 4) + up(100 * 4 * 4)  # a score per entry and head, a sum per row and head
