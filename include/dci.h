@@ -520,7 +520,7 @@ typedef struct {
   int64_t out_stride;
   float* lse;              /* device [n_rows, n_heads] (nullable)                                      */
   const float* bias;       /* device [n_edges, bias_heads] (nullable)                                  */
-  int32_t bias_heads;      /* 1 (shared by the heads) or n_heads; 0 without bias                       */
+  int32_t bias_heads;      /* 1 (shared by the heads) or n_heads; 0 without bias (any of them where n_edges = 0) */
 } dci_attn;
 
 /* Workspace of an attention call (accumulate as for dci_attn_cached): lists of more than 64 entries are worked on in pieces, which

@@ -418,8 +418,8 @@ int32_t check_rows(dci_ctx* ctx, const dci_kv_cache* cache, const int32_t* slots
 // runs, the slots that are hit have the highest bit of their weight set.
 // Nothing waits for another workgroup: what a kernel leaves is looked through by every workgroup of the next (the counts of a digit, the sums of at
 // most 1,024 tiles).  What bounds it: seven launches (eight for large caches) one after the other, each a few dependent reads long, and for large
-// batches the random lines of remap, weights and nodes.  400,000 nodes on a million slots take 89 us: 23 of them the look-up (0.55 million lines that
-// L2 does not have, 24 a nanosecond, and as many atomics), 11 the first digit, 12 the other two, 10 numbering, 15 giving, 8 the slots; 3,000 nodes
+// batches the random lines of remap, weights and nodes.  400,000 nodes on a million slots take 87 us: 21 of them the look-up (0.55 million lines that
+// L2 does not have, 26 a nanosecond, and 0.24 million atomics), 11 the first digit, 12 the other two, 10 numbering, 15 giving, 8 the slots; 3,000 nodes
 // on 65,536 slots take 37 us in launches of 3 to 7 us.
 
 constexpr int kDigit = 13, kBins = 1 << kDigit, kDigits = 3;
@@ -513,7 +513,7 @@ __global__ __launch_bounds__(kAdmitBlock) void k_admit_lookup(const Admit a) {
   const long long v = a.nodes[i];
   if (v < 0 || v >= a.num_nodes) return;
   const int s = a.remap[v];  // a claim that has just been made may or may not show: either way it is no slot
-  if (s >= 0 && (unsigned)s < a.n_slots) atomicOr(a.weight + s, kHit);
+  if (s >= 0 && (unsigned)s < a.n_slots) a.weight[s] |= kHit;  // (whoever else has the node writes the same)
   else atomicMin(a.remap + v, kClaim + (int)i);
 }
 
