@@ -62,6 +62,7 @@ struct Attn {
   float* scores;     // [n_edges, heads], accumulating only
   unsigned long long* weight;
   int lh_log2, p_log2, r_log2;  // lanes to a head, to an entry; lane groups to a row
+  bool ragged;                  // dense rows whose heads do not fill those lanes: columns of others, or none, are read as well
   int wave_heads;               // key heads to a wavefront
   int passes;                   // wavefronts that share a row's key heads and their groups
   int gq_passes;                // of them, those that share a group
@@ -182,6 +183,35 @@ __device__ __forceinline__ int first_source(const Attn& a, const Place& pl, long
   return t < entries(a, e0, e1) ? a.src[e0 + t] : -1;
 }
 
+// Which columns of a piece of a dense row are the lane's own, as masks of its words.  (q has a 0 for the others, but 0 times an infinite key is no number.
+// The masks cost 24,576 rows of nine entries up to 5 % where heads do not fill their lanes, eight 16-bit heads of 40 on four 36 -> 37 us, and 1 %
+// on average where they do; made anew for each entry, as those of 32-bit rows are, they cost 16-bit ones up to 13 %.)
+template <int TYPE>
+struct Own {
+  static constexpr int kMasks = TYPE == DCI_F32 ? 1 : 4;
+  unsigned at[kMasks];  // of fp32 rows the first of them: a mask to a word would take registers that are not there
+
+  __device__ __forceinline__ void set(const Attn& a, const Place& pl, int j) {
+    bool some;
+    int skip;
+    (void)first_column<TYPE, true>(a, pl, j, &some, &skip);
+    const int first = some ? skip : kPiece<TYPE>;
+    if (TYPE == DCI_F32) at[0] = (unsigned)first;
+#pragma unroll
+    for (int i = 0; i < kMasks && TYPE != DCI_F32; ++i) {
+      at[i] = first <= 2 * i ? ~0u : first == 2 * i + 1 ? 0xFFFF0000u : 0u;
+      asm volatile("" : "+v"(at[i]));
+    }
+  }
+  __device__ __forceinline__ uint4 of(uint4 w) const {
+    if (TYPE != DCI_F32) return make_uint4(w.x & at[0], w.y & at[kMasks > 1 ? 1 : 0], w.z & at[kMasks > 2 ? 2 : 0], w.w & at[kMasks > 3 ? 3 : 0]);
+    int first = (int)at[0];
+    asm volatile("" : "+v"(first));
+    auto own = [&](int i) { return (unsigned)((first - i - 1) >> 31); };
+    return make_uint4(w.x & own(0), w.y & own(1), w.z & own(2), w.w & own(3));
+  }
+};
+
 // Entries [e0, e1) of one row into st (source0: their first_source): those of group `sub` are every (1 << r_log2)-th from e0 + sub on.  Returns what the lane's entry of the last
 // P << r_log2 named (there are no more where that is used).  stash (nullable): LDS for the scores, entry by entry of the wavefront; scores (nullable):
 // memory for them, entry by entry of the call.
@@ -204,6 +234,11 @@ __device__ __forceinline__ int attend(const Attn& a, const Place& pl, long long 
     bool some;
     int skip;
     offset[j] = (TYPE == kE4M3 ? cached_column(a, pl) : first_column<TYPE, WIDE>(a, pl, j, &some, &skip)) * type_bytes(TYPE);
+  }
+  Own<TYPE> own[Chunk<TYPE, C>::kWords];
+  if (TYPE != kE4M3 && WIDE) {
+#pragma unroll
+    for (int j = 0; j < Chunk<TYPE, C>::kWords; ++j) own[j].set(a, pl, j);
   }
   if (TYPE == kE4M3) {
     k0 += offset[0];
@@ -257,6 +292,10 @@ __device__ __forceinline__ int attend(const Attn& a, const Place& pl, long long 
       float z[U][GQ];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
+        if (TYPE != kE4M3 && WIDE && a.ragged) {  // q has a 0 for the others, but 0 times an infinity is no number
+#pragma unroll
+          for (int j = 0; j < Chunk<TYPE, C>::kWords; ++j) kc[u].w[j] = own[j].of(kc[u].w[j]);
+        }
 #pragma unroll
         for (int g = 0; g < GQ; ++g) z[u][g] = 0.f;
 #pragma unroll
@@ -1147,6 +1186,7 @@ int32_t attn(dci_ctx* ctx, const dci_attn& t, int type, Attn a, bool accumulate)
   a.part_ml = parts.ml;
   a.part_acc = parts.acc;
   a.lh_log2 = s.lh_log2;
+  a.ragged = type != kE4M3 && s.wide && t.head_dim != kCols<DCI_F32> << s.lh_log2;
   a.p_log2 = s.p_log2;
   a.wave_heads = s.wave_heads;
   a.passes = s.passes;

@@ -1,0 +1,61 @@
+"""Attention over lists where its arithmetic and its launches end: infinite keys at every way that a head's columns lie on lanes.
+
+Tolerances are those of attention_reference.attend."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from tests import attention_reference as ref
+from tests.test_gpu_attention import TYPES, check, lists, rounded
+
+pytestmark = pytest.mark.gpu
+
+
+def dev(a):
+    return None if a is None else torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+# widths that fill their lanes (8, 64, 256), leave lanes without columns (24, 40, 80, 96) or end inside a piece (9, 41, 97, 200)
+@pytest.mark.parametrize("dim", [8, 9, 24, 40, 41, 64, 80, 96, 97, 200, 256])
+@pytest.mark.parametrize("heads,kv,dtype,bias_heads", [(3, 3, "fp32", 0), (4, 2, "fp32", 4), (8, 2, "fp32", 0), (2, 2, "bf16", 1), (4, 2, "fp16", 0),
+                                                       (4, 1, "fp16", 4)])
+def test_infinite_keys_of_dense_rows(dim, heads, kv, dtype, bias_heads):
+    """A key whose score is -inf has weight 0, wherever in the row its infinity stands; one whose score is none makes the row none."""
+    import paper_2503_01281_amd as dci
+    ctx = dci.Context(0)
+    rng = np.random.default_rng(dim * 100 + heads)
+    sources, lengths = 120, [5, 0, 64, 17, 130, 1, 300, 40]
+    indptr, src = lists(lengths, sources, rng)
+    src[indptr[:-1][np.array(lengths) > 0]] = 0  # every list begins with a source whose key is finite
+    n = len(lengths)
+    q, k, v = (rounded(rng.standard_normal((m, h, dim)).astype(np.float32), dtype) for m, h in ((n, heads), (sources, kv), (sources, kv)))
+    q = q.abs() + 0.25  # positive: a key of -inf gives a score of -inf
+    gone = np.zeros(sources, dtype=bool)
+    for s in range(1, sources):
+        if rng.random() < 0.4:
+            gone[s] = True
+            k[s, :, rng.integers(max(0, dim - 17), dim) if s % 3 else rng.integers(dim)] = -math.inf
+    bias = rng.standard_normal((src.size, bias_heads)).astype(np.float32) if bias_heads else None
+    where = np.where(gone[src], -1, src).astype(np.int64)
+    finite = torch.where(torch.isinf(k), torch.zeros_like(k), k)
+    scale = 1.0 / math.sqrt(dim)
+    want = ref.attend(q.double().numpy(), finite.double().numpy(), v.double().numpy(), indptr, where, np.float64(np.float32(scale)),
+                      None if bias is None else bias.astype(np.float64))
+
+    def call():
+        out, lse = torch.full((n, heads, dim), 7.0, dtype=TYPES[dtype], device="cuda"), torch.full((n, heads), 7.0, device="cuda")
+        dci.dci_attn_forward(ctx, q.cuda(), k.cuda(), v.cuda(), dev(indptr), dev(src), out, scale, lse=lse, bias=dev(bias))
+        ctx.sync()
+        return out, lse
+
+    out, lse = call()
+    check(out, lse, want, n, dtype)
+    s = int(src[indptr[2] + 3])  # a source of row 2: infinities of both signs, no score
+    if dim > 1 and s != 0:
+        k[s, :, dim - 1], k[s, :, 0] = -math.inf, math.inf
+        named = np.array([s in src[indptr[i]:indptr[i + 1]] for i in range(n)])
+        out, lse = call()
+        assert torch.isnan(out.float()).all(-1).cpu().numpy()[named].all() and torch.isnan(lse).cpu().numpy()[named].all()
+        assert not torch.isnan(out.float()).any(-1).cpu().numpy()[~named].any()
