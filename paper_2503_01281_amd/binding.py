@@ -599,7 +599,7 @@ def dci_attn_cached(ctx: Context, q: torch.Tensor, cache: KvCache, indptr: torch
     need = ctx.lib.dci_attn_workspace_bytes(C.byref(a), int(accumulate))
     if need:
         ctx.ensure_workspace(need)
-    at = _ptr(slots) if slots is None or slots.numel() else _ptr(indptr)  # without sources: read by nobody, but not null, which has a meaning
+    at = _ptr(slots) if slots is None or slots.numel() else _ptr(indptr)  # without sources: read by nobody (dci_attn_cached sees to it), but not null
     ctx.check(ctx.lib.dci_attn_cached(ctx.handle, C.byref(a), C.byref(cache.c), at, int(accumulate)))
 
 

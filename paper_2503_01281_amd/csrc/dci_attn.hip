@@ -1239,7 +1239,7 @@ int32_t attn(dci_ctx* ctx, const dci_attn& t, int type, Attn a, bool accumulate)
     if (s.n_chunks) {
       hipLaunchKernelGGL(k_attn_join, dim3((unsigned)((by_row ? t.n_rows : s.n_chunks) * t.n_heads)), dim3(kAttnBlock), 0, ctx->stream, a, by_row);
       DCI_LAUNCH_CHECK(ctx);
-      if (accumulate) {
+      if (accumulate && a.n_src > 0) {  // (without sources nobody has written scores)
         hipLaunchKernelGGL(k_attn_weights, dim3((unsigned)((s.n_chunks + kAttnWaves - 1) / kAttnWaves)), dim3(kAttnBlock), 0, ctx->stream, a);
         DCI_LAUNCH_CHECK(ctx);
       }
@@ -1298,7 +1298,8 @@ int32_t dci_attn_cached(dci_ctx* ctx, const dci_attn* attn, const dci_kv_cache* 
   if (attn->n_rows == 0) return DCI_OK;
   const int width = dci::kv_width(cache->head_dim);
   dci::Attn a = {};
-  a.slots = slots;
+  // Lanes whose entry names no source read the first slot all the same; without sources there is none, and they read what is there instead.
+  a.slots = slots && attn->n_src == 0 ? reinterpret_cast<const int32_t*>(attn->indptr) : slots;
   a.n_at = (unsigned)cache->n_slots;
   a.n_src = slots ? (unsigned)attn->n_src : a.n_at;
   a.k = reinterpret_cast<const char*>(cache->codes);

@@ -1,4 +1,5 @@
-"""Attention over lists where its arithmetic and its launches end: infinite keys at every way that a head's columns lie on lanes.
+"""Attention over lists where its arithmetic and its launches end: infinite keys at every way that a head's columns lie on lanes, no
+sources.
 
 Tolerances are those of attention_reference.attend."""
 import math
@@ -59,3 +60,29 @@ def test_infinite_keys_of_dense_rows(dim, heads, kv, dtype, bias_heads):
         out, lse = call()
         assert torch.isnan(out.float()).all(-1).cpu().numpy()[named].all() and torch.isnan(lse).cpu().numpy()[named].all()
         assert not torch.isnan(out.float()).any(-1).cpu().numpy()[~named].any()
+
+
+@pytest.mark.parametrize("heads,kv,dim", [(4, 1, 64), (16, 2, 128), (3, 1, 256), (4, 4, 64), (8, 2, 32)])
+@pytest.mark.parametrize("rows,each", [(1, 65), (3, 700), (40, 90)])
+def test_long_lists_without_sources(heads, kv, dim, rows, each):
+    """Slots without elements: entries, long lists of heads that share keys among them, name nothing."""
+    import ctypes as C
+
+    import paper_2503_01281_amd as dci
+    from paper_2503_01281_amd import binding as b
+    from tests.test_gpu_attention import make_cache
+    ctx = dci.Context(0)
+    cache, _ = make_cache(dci, 50, kv, dim, 16, np.random.default_rng(rows))
+    before = cache.weight.clone()
+    indptr = torch.arange(0, rows * each + 1, each, device="cuda")
+    src = (torch.arange(rows * each, dtype=torch.int32) % 50).cuda()
+    q = torch.randn(rows, heads, dim, device="cuda")
+    for through in ("binding", "library"):
+        out, lse = torch.full_like(q, 7.0), torch.full((rows, heads), 7.0, device="cuda")
+        if through == "binding":
+            dci.dci_attn_cached(ctx, q, cache, indptr, src, out, 0.125, slots=torch.empty(0, dtype=torch.int32, device="cuda"), lse=lse, accumulate=True)
+        else:
+            a = b._attn_args(q, kv, 0, indptr, src, out, 0.125, lse, None, None, 0)
+            ctx.check(ctx.lib.dci_attn_cached(ctx.handle, C.byref(a), C.byref(cache.c), src.data_ptr(), 1))  # not null, and none of it is a slot
+        ctx.sync()
+        assert (out == 0).all() and torch.isneginf(lse).all() and torch.equal(cache.weight, before)
