@@ -1043,6 +1043,7 @@ struct Split {
   int chunk;
   int64_t n_chunks;
 };
+constexpr int64_t kMaxGroups = 0xFFFFFFFFll / kAttnBlock;  // workgroups to a launch, whose lanes are counted in 32 bits
 constexpr int64_t kWantedWaves = 4096, kFewWaves = 1024;  // 16 and four to a compute unit
 constexpr int kStashHeads = 32;  // query heads of a wavefront, at most, with weights: 40 KB of scores to a workgroup, four workgroups to a compute unit
 
@@ -1072,6 +1073,8 @@ Split split_of(const dci_attn& t, int type, bool accumulate) {
   // 37,000 entries of eight 16-bit heads of 128 on two take 46 us in chunks of 16, 38 in 32, 37 in 64.
   s.chunk = s.matrix ? 32 : 16;
   while (s.chunk < 512 && t.n_edges / s.chunk * waves > (s.chunk < 64 ? kFewWaves : kWantedWaves)) s.chunk *= 2;
+  // Longer ones where the join, a workgroup to a chunk and head, would have more workgroups than a launch may have; no other launch has more.
+  while ((t.n_edges + s.chunk - 1) / s.chunk * t.n_heads > kMaxGroups) s.chunk *= 2;
   const int64_t longest = t.max_list > 0 && t.max_list < t.n_edges ? t.max_list : t.n_edges;
   s.n_chunks = longest > kShort ? (t.n_edges + s.chunk - 1) / s.chunk : 0;
   return s;
@@ -1157,8 +1160,6 @@ int32_t attn(dci_ctx* ctx, const dci_attn& t, int type, Attn a, bool accumulate)
     ctx->req_workspace = ar.off;
     return fail(ctx, DCI_ERR_CAPACITY, "workspace holds %zu bytes, this attention call needs %zu", ctx->ws_bytes, ar.off);
   }
-  if (s.n_chunks * t.n_heads * 4 > 0x7FFFFFFFll || t.n_rows * s.passes > 0xF0000000ll)
-    return fail(ctx, DCI_ERR_UNSUPPORTED, "attention: too many list entries and heads for one call");
   const int64_t b = type_bytes(t.dtype);
   a.n_rows = t.n_rows;
   a.n_dev = reinterpret_cast<const long long*>(t.n_dev);

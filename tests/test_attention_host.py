@@ -90,3 +90,15 @@ def test_the_reference_writes_and_admits():
     slots, fresh, fresh_slots, counts = ref.admit(remap, node, weight, np.array([3, 0, 3, 1]))
     assert slots.tolist() == [1, 0, 1, -1] and fresh.tolist() == [0, -1, -1, -1] and fresh_slots.tolist() == [1, -1, -1, -1]
     assert counts.tolist() == [1, 2, 1, 1] and remap.tolist() == [0, -1, -1, 1] and node.tolist() == [0, 3] and weight.tolist() == [5, 1]
+
+
+@pytest.mark.parametrize("heads,kv,dim", [(128, 128, 16), (128, 1, 64), (32, 8, 128), (4, 4, 64), (1, 1, 1)])
+@pytest.mark.parametrize("edges", [10 ** 6, 67_225_600, 2 ** 28 + 1, 10 ** 9, 2 ** 33 + 7, 2 ** 38])
+def test_no_launch_has_more_lanes_than_32_bits_count(lib, heads, kv, dim, edges):
+    """The pieces of long lists, two to a chunk and head, are joined by a workgroup of 256 lanes to a chunk and head."""
+    from paper_2503_01281_amd import binding as b
+    a = b._Attn(n_rows=2 ** 31 - 1, n_edges=edges, n_src=10, max_list=0, n_heads=heads, kv_heads=kv, head_dim=dim)
+    piece = 2 * 4 + -(-dim // 16) * 16 * 4
+    chunks = lib.dci_attn_workspace_bytes(C.byref(a), 0) // (2 * heads * piece)
+    assert 0 < chunks * heads * 256 < 2 ** 32
+    assert chunks * 2 ** 22 >= edges  # and a chunk stays one that a wavefront goes through in milliseconds

@@ -1,5 +1,5 @@
 """Attention over lists where its arithmetic and its launches end: infinite keys at every way that a head's columns lie on lanes, no
-sources.
+sources, more pieces than one launch has workgroups for.
 
 Tolerances are those of attention_reference.attend."""
 import math
@@ -86,3 +86,26 @@ def test_long_lists_without_sources(heads, kv, dim, rows, each):
             ctx.check(ctx.lib.dci_attn_cached(ctx.handle, C.byref(a), C.byref(cache.c), src.data_ptr(), 1))  # not null, and none of it is a slot
         ctx.sync()
         assert (out == 0).all() and torch.isneginf(lse).all() and torch.equal(cache.weight, before)
+
+
+def test_more_chunks_and_heads_than_a_launch_has_workgroups():
+    """67 million entries, 128 heads: with chunks of 512 the join would need 16.8 million workgroups, 2^32 lanes and more."""
+    import paper_2503_01281_amd as dci
+    ctx = dci.Context(0)
+    rng = np.random.default_rng(12)
+    n, each, heads, dim, sources = 131_300, 512, 128, 16, 100
+    gen = torch.Generator(device="cuda").manual_seed(12)
+    indptr = torch.arange(0, (n + 1) * each, each, device="cuda") - each // 2  # lists that begin in the middle of a chunk
+    indptr[0] = 0
+    src = torch.randint(sources, (int(indptr[-1]),), generator=gen, device="cuda", dtype=torch.int32)
+    q = torch.randn(n, heads, dim, generator=gen, device="cuda", dtype=torch.bfloat16)
+    k, v = (torch.randn(sources, heads, dim, generator=gen, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    out, lse = torch.full_like(q, float("nan")), torch.full((n, heads), float("nan"), device="cuda")
+    dci.dci_attn_forward(ctx, q, k, v, indptr, src, out, 0.25, lse=lse)
+    ctx.sync()
+    assert torch.isfinite(lse).all() and torch.isfinite(out).all()
+    for i in np.unique(np.concatenate([[0, 1, n - 2, n - 1, 2 ** 17 - 1, 2 ** 17], rng.integers(0, n, 3)])):
+        b, e = int(indptr[i]), int(indptr[i + 1])
+        want = ref.attend(q[i:i + 1].double().cpu().numpy(), k.double().cpu().numpy(), v.double().cpu().numpy(), [0, e - b],
+                          src[b:e].cpu().numpy().astype(np.int64), 0.25)
+        check(out[i:i + 1], lse[i:i + 1], want, 1, "bf16")
