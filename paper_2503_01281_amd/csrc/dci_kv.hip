@@ -50,6 +50,7 @@ struct KvWrite {
   float* scales;
   long long n_slots;
   int block_log2, kv_heads, dim, lh_log2;
+  unsigned first_turn;  // of this launch
   unsigned* host_flag;
 };
 
@@ -188,7 +189,7 @@ __global__ __launch_bounds__(kKvBlock) void k_kv_write(const KvWrite a) {
   const unsigned unit = blockIdx.x * (unsigned)kKvWaves + wave, turn = unit / (unsigned)a.kv_heads;
   const int head = (int)(unit - turn * a.kv_heads);
   const int lh = 1 << a.lh_log2, at_once = kWave >> a.lh_log2, tile = T * at_once;
-  const long long i0 = (long long)turn * tile;
+  const long long i0 = ((long long)a.first_turn + turn) * tile;
   const long long n = a.n_dev ? min(a.n_max, max(0ll, *a.n_dev)) : a.n_max;
   __shared__ unsigned peaks[kKvWaves][2][kWave];
   if (i0 >= n) return;
@@ -883,14 +884,20 @@ int32_t dci_kv_write(dci_ctx* ctx, const dci_kv_cache* cache, const int32_t* slo
   const int at_once = dci::kWave >> a.lh_log2, most = n_max >= cache->n_slots / 2 ? 8 : 4;
   int tiles = 1;
   while (tiles < most && tiles * at_once < cache->block) tiles *= 2;
-  const int64_t waves = (n_max + tiles * at_once - 1) / (tiles * at_once) * cache->kv_heads;
-  const int64_t grid = (waves + dci::kKvWaves - 1) / dci::kKvWaves;
-  if (waves > 0x7FFFFFFFll) return dci::fail(ctx, DCI_ERR_UNSUPPORTED, "key/value rows: too many rows and heads for one call");
+  // A launch's lanes are counted in 32 bits, and one of more runs what is left of their number beyond: turns go to as many launches as that takes, each
+  // a whole number of workgroups.
+  const int64_t turns = (n_max + tiles * at_once - 1) / (tiles * at_once);
+  const int64_t most_turns = (0xFFFFFFFFll / dci::kKvBlock) / cache->kv_heads * dci::kKvWaves;
   dci::Timed timed(ctx, DCI_K_KV);
-  if (dtype == DCI_F32) dci::launch_write<DCI_F32>(tiles, a, (unsigned)grid, ctx->stream);
-  else if (dtype == DCI_BF16) dci::launch_write<DCI_BF16>(tiles, a, (unsigned)grid, ctx->stream);
-  else dci::launch_write<DCI_F16>(tiles, a, (unsigned)grid, ctx->stream);
-  DCI_LAUNCH_CHECK(ctx);
+  for (int64_t first = 0; first < turns; first += most_turns) {
+    a.first_turn = (unsigned)first;
+    const int64_t waves = (turns - first < most_turns ? turns - first : most_turns) * cache->kv_heads;
+    const unsigned grid = (unsigned)((waves + dci::kKvWaves - 1) / dci::kKvWaves);
+    if (dtype == DCI_F32) dci::launch_write<DCI_F32>(tiles, a, grid, ctx->stream);
+    else if (dtype == DCI_BF16) dci::launch_write<DCI_BF16>(tiles, a, grid, ctx->stream);
+    else dci::launch_write<DCI_F16>(tiles, a, grid, ctx->stream);
+    DCI_LAUNCH_CHECK(ctx);
+  }
   return DCI_OK;
 }
 
