@@ -543,9 +543,9 @@ int32_t dci_attn_cached(dci_ctx* ctx, const dci_attn* attn, const dci_kv_cache* 
 int32_t dci_kv_clear(dci_ctx* ctx, const dci_kv_cache* cache);
 
 /* Writes rows of keys and values into the cache.  slots: device int32 [n_max], STRICTLY ASCENDING; entries outside [0, n_slots) are
- * skipped, with their rows, and stand behind all others (fresh_slots of dci_kv_admit ends in such entries).  The number of rows is
- * *n_dev (device int64) where n_dev is not NULL, n_max its bound.  k, v: device rows of `dtype`, row i, head h at i * stride + h *
- * head_dim.
+ * skipped, with their rows, which need not exist, and stand behind all others (fresh_slots of dci_kv_admit ends in such entries).
+ * The number of rows is *n_dev (device int64) where n_dev is not NULL, n_max its bound.  k, v: device rows of `dtype`, row i, head h
+ * at i * stride + h * head_dim.
  * For every block that the call writes to, head and kind: need = the least e with max |x| <= 448 * 2^e over the finite numbers written,
  * within [-100, 119]; the block's scale becomes 2^need where the call writes every slot of the block or its scale is 0, and
  * 2^max(need, old) otherwise.  Numbers are divided by the scale and rounded to the nearest e4m3 (ties to even; beyond 448 to
