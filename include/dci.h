@@ -551,8 +551,8 @@ int32_t dci_kv_clear(dci_ctx* ctx, const dci_kv_cache* cache);
  * 2^max(need, old) otherwise.  Numbers are divided by the scale and rounded to the nearest e4m3 (ties to even; beyond 448 to
  * 448); infinities and NaN become NaN.  Where the scale grows, the block's other slots are rounded anew: exactly, but for what
  * falls below the smallest normal e4m3 (2^-6 of the scale).
- * A call whose slots do not ascend so is an error that the next dci_sync reports (DCI_ERR_INVALID_ARG); what the blocks concerned
- * then hold is not specified. */
+ * A call whose slots do not ascend so is an error that the next dci_sync reports (DCI_ERR_INVALID_ARG; together with a batch that was
+ * voided, DCI_ERR_HIP and a message that names both); what the blocks concerned then hold is not specified. */
 int32_t dci_kv_write(dci_ctx* ctx, const dci_kv_cache* cache, const int32_t* slots, int64_t n_max, const int64_t* n_dev, int32_t dtype,
                      const void* k, int64_t k_stride, const void* v, int64_t v_stride);
 /* Reads rows back: row i of k and v (device, `dtype`) = what slot slots[i] holds, rounded to the type; rows of entries outside

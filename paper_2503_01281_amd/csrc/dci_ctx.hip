@@ -54,14 +54,16 @@ int32_t fill_bytes(dci_ctx* ctx, void* p, size_t bytes, uint32_t pattern) {
 }
 
 int32_t check_device_flag(dci_ctx* ctx) {
-  if (ctx->host_flag && *ctx->host_flag != 0u) {
-    const unsigned flag = *ctx->host_flag;
-    *ctx->host_flag = 0u;
-    if (flag == 2u) return fail(ctx, DCI_ERR_INVALID_ARG, "dci_kv_write: slots must be strictly ascending, entries outside the cache behind all others");
+  if (!ctx->host_flag) return DCI_OK;
+  const bool voided = ctx->host_flag[0] != 0u, unordered = ctx->host_flag[1] != 0u;
+  ctx->host_flag[0] = ctx->host_flag[1] = 0u;
+  static const char slots[] = "dci_kv_write: slots must be strictly ascending, entries outside the cache behind all others";
+  if (voided)
     return fail(ctx, DCI_ERR_HIP,
                 "relabel scan timed out: a tile of the frontier scan waited longer than the spin limit for its "
-                "predecessors; the batch was voided (sizes zeroed) and its outputs must not be used");
-  }
+                "predecessors; the batch was voided (sizes zeroed) and its outputs must not be used%s%s",
+                unordered ? "; and " : "", unordered ? slots : "");
+  if (unordered) return fail(ctx, DCI_ERR_INVALID_ARG, "%s", slots);
   return DCI_OK;
 }
 
@@ -94,7 +96,7 @@ int32_t dci_create(dci_ctx** out, int32_t device, void* hip_stream, void* worksp
     if (e == hipSuccess) {
       ctx->host_flag = static_cast<unsigned*>(p);
       ctx->host_scal = reinterpret_cast<unsigned long long*>(static_cast<char*>(p) + 64);
-      *ctx->host_flag = 0u;
+      ctx->host_flag[0] = ctx->host_flag[1] = 0u;
     }
   }
   if (e != hipSuccess) {

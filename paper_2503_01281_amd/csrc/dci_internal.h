@@ -27,7 +27,8 @@ struct dci_ctx {
   hipEvent_t* t_events = nullptr;  // 2 * DCI_TIMING_MAX_LAUNCHES, created on first enable
   int8_t* t_class = nullptr;
   int t_used = 0;
-  unsigned* host_flag = nullptr;  // pinned host word (64 bytes): a kernel raises it when a batch had to be voided
+  // pinned host words (64 bytes) that kernels raise: [0] when a batch had to be voided, [1] when a key/value write's slots did not ascend
+  unsigned* host_flag = nullptr;
   unsigned long long* host_scal = nullptr;  // eight pinned words behind it: what dci_fill_caches reads back
   unsigned relabel_spin_limit = 1u << 24;  // DCI_OPT_RELABEL_SPIN_LIMIT
   unsigned test_first_ticket = 0;          // DCI_OPT_TEST_RELABEL_FIRST_TICKET
@@ -149,7 +150,7 @@ __device__ __forceinline__ unsigned long long wave_sum_u64(unsigned long long x)
 __global__ void k_fill_u32x4(uint4* __restrict__ p, size_t n16, uint32_t pattern);
 
 int32_t fill_bytes(dci_ctx* ctx, void* p, size_t bytes, uint32_t pattern);
-// After a wait on the context's stream: reports (and clears) a failure that a kernel flagged.
+// After a wait on the context's stream: reports (and clears) what kernels have flagged, all of it.
 int32_t check_device_flag(dci_ctx* ctx);
 // What the closing workgroups of a batch do (close_batch)
 struct CloseArgs {

@@ -218,7 +218,7 @@ __global__ __launch_bounds__(kKvBlock) void k_kv_write(const KvWrite a) {
   const int behind = slot_at(i0 + tile);
   peaks[wave][0][lane] = peaks[wave][1][lane] = 0;
   const bool is_first = s >= 0 && (before < 0 || (before >> a.block_log2) != (s >> a.block_log2));
-  if (s >= 0 && i0 + lane > 0 && (before < 0 || before >= s)) *a.host_flag = 2u;  // not ascending: dci_sync says so
+  if (s >= 0 && i0 + lane > 0 && (before < 0 || before >= s)) *a.host_flag = 1u;  // not ascending: dci_sync says so
   const unsigned long long firsts = __ballot(is_first);
   if (!firsts) return;
   const int last_first = kWave - 1 - __builtin_clzll(firsts);
@@ -878,7 +878,7 @@ int32_t dci_kv_write(dci_ctx* ctx, const dci_kv_cache* cache, const int32_t* slo
   a.kv_heads = cache->kv_heads;
   a.dim = cache->head_dim;
   a.lh_log2 = dci::log2_up((cache->head_dim + dci::kChunk - 1) / dci::kChunk);
-  a.host_flag = ctx->host_flag;
+  a.host_flag = ctx->host_flag + 1;
   // Entries to a wavefront: a block's, as far as four times the rows that it has lanes for go, eight times where many blocks may be written whole (a
   // block that does not fit is read twice).  Heads of 128, blocks of 64, 16-bit rows: 200,000 of 200,000 slots 469 us with eight and 611 with four,
   // 20,000 of them 270 and 256.

@@ -1,5 +1,5 @@
 """The 8-bit key/value cache where its launches end: more rows and heads than one launch has lanes for, entries without
-rows.  Codes and scales are defined to the bit."""
+rows, two errors at a time.  Codes and scales are defined to the bit."""
 import ctypes as C
 
 import numpy as np
@@ -53,3 +53,31 @@ def test_entries_outside_the_cache_need_no_rows(n, heads, dim, dtype, block):
     ctx.sync()
     ref.write(held, exponents, slots[:n], k.double().numpy(), v.double().numpy(), n_slots, block)
     compare(cache, held, exponents)
+
+
+@pytest.mark.parametrize("order", [("batch", "write"), ("write", "batch"), ("batch",), ("write",)])
+def test_a_voided_batch_and_bad_slots_are_both_reported(order, tiny):
+    """Two errors between two waits: the one does not hide the other.  The batch is voided as by a wait that ends: tiles numbered from 1 wait for
+    tile 0, 200 polls long."""
+    import paper_2503_01281_amd as dci
+    from tests import gpu_util as gu
+    w, n = tiny["w"], 600
+    ctx = dci.Context(0, workspace_bytes=64 << 20)
+    graph = gu.make_graph(tiny["indptr"], tiny["indices"], tiny["feat"])
+    blk = dci.Blocks(ctx, w.num_nodes, n, w.fanouts)
+    cache = dci.KvCache(ctx, 64, 2, 32, 16)
+    rows, seeds, bad = torch.ones(2, 2, 32, device="cuda"), gu.dev(tiny["seeds"][:n]), dev(np.array([6, 5], dtype=np.int32))
+    ctx.set_option(dci.DCI_OPT_RELABEL_SPIN_LIMIT, 200)
+    ctx.set_option(dci.DCI_OPT_TEST_RELABEL_FIRST_TICKET, 1)
+    for what in order:
+        if what == "batch":
+            dci.dci_sample_khop(ctx, graph, None, seeds, 0, w.fanouts, w.rng_seed, blk)
+        else:
+            dci.dci_kv_write(ctx, cache, bad, rows, rows)
+        torch.cuda.synchronize()
+    with pytest.raises(dci.DciError) as e:
+        ctx.sync()
+    assert ("relabel scan timed out" in str(e.value) and "must not be used" in str(e.value)) == ("batch" in order)
+    assert ("strictly ascending" in str(e.value)) == ("write" in order)
+    assert e.value.code == (-3 if "batch" in order else -1)
+    ctx.sync()  # reported once
