@@ -525,7 +525,8 @@ typedef struct {
 
 /* Workspace of an attention call (accumulate as for dci_attn_cached): lists of more than 64 entries are worked on in pieces, which
  * are joined from there; with accumulate their scores are kept there.  0 where max_list says that there are no such lists.  It
- * depends on n_rows, n_edges, max_list, dtype, heads, head_dim, bias and accumulate only. */
+ * depends on n_rows, n_edges, max_list, dtype, heads, head_dim, bias and accumulate only, and does not fall as the first three grow
+ * (max_list 0 being the largest): what a program's largest call needs does for all its smaller ones. */
 size_t dci_attn_workspace_bytes(const dci_attn* attn, int32_t accumulate);
 
 /* Attention over dense rows (a model's later layers): source s, key head h at k + s * k_stride + h * head_dim, v likewise; strides in

@@ -1042,6 +1042,7 @@ struct Split {
   bool wide;  // heads of 16 bytes at least: read and written 16 at a time
   int chunk;
   int64_t n_chunks;
+  int64_t most_chunks;  // that this call or one of fewer entries has, which may be cut shorter
 };
 constexpr int64_t kMaxGroups = 0xFFFFFFFFll / kAttnBlock;  // workgroups to a launch, whose lanes are counted in 32 bits
 constexpr int64_t kWantedWaves = 4096, kFewWaves = 1024;  // 16 and four to a compute unit
@@ -1071,25 +1072,30 @@ Split split_of(const dci_attn& t, int type, bool accumulate) {
   // each, take 309 us for 261).  Shorter ones (16 or 32; a step of k_attn_groups is 32 entries) where that leaves only a few to a compute unit: 28,000
   // entries of seven 32-bit heads of 64 take 48 us in chunks of 32 and 55 in chunks of 64.  With more wavefronts the pieces cost more than they give:
   // 37,000 entries of eight 16-bit heads of 128 on two take 46 us in chunks of 16, 38 in 32, 37 in 64.
-  s.chunk = s.matrix ? 32 : 16;
-  while (s.chunk < 512 && t.n_edges / s.chunk * waves > (s.chunk < 64 ? kFewWaves : kWantedWaves)) s.chunk *= 2;
+  int64_t most = 0;
+  for (s.chunk = s.matrix ? 32 : 16; s.chunk < 512; s.chunk *= 2) {
+    const int64_t wanted = s.chunk < 64 ? kFewWaves : kWantedWaves;
+    if (t.n_edges / s.chunk * waves <= wanted) break;
+    if (wanted / waves + 1 > most) most = wanted / waves + 1;
+  }
   // Longer ones where the join, a workgroup to a chunk and head, would have more workgroups than a launch may have; no other launch has more.
-  while ((t.n_edges + s.chunk - 1) / s.chunk * t.n_heads > kMaxGroups) s.chunk *= 2;
+  for (; (t.n_edges + s.chunk - 1) / s.chunk * t.n_heads > kMaxGroups; s.chunk *= 2) most = kMaxGroups / t.n_heads;
   const int64_t longest = t.max_list > 0 && t.max_list < t.n_edges ? t.max_list : t.n_edges;
   s.n_chunks = longest > kShort ? (t.n_edges + s.chunk - 1) / s.chunk : 0;
+  s.most_chunks = s.n_chunks && most > s.n_chunks ? most : s.n_chunks;
   return s;
 }
 
 struct Parts {
   float *scores = nullptr, *all_lse = nullptr, *ml = nullptr, *acc = nullptr;
 };
-Parts take_parts(Arena& ar, const dci_attn& t, const Split& s, bool accumulate) {
+Parts take_parts(Arena& ar, const dci_attn& t, int64_t n_chunks, bool accumulate) {
   Parts p;
-  if (s.n_chunks) {
+  if (n_chunks) {
     if (accumulate) p.scores = ar.take<float>((size_t)t.n_edges * t.n_heads);
     if (accumulate) p.all_lse = ar.take<float>((size_t)t.n_rows * t.n_heads);
-    p.ml = ar.take<float>((size_t)s.n_chunks * 2 * t.n_heads * 2);
-    p.acc = ar.take<float>((size_t)s.n_chunks * 2 * t.n_heads * kv_width(t.head_dim));
+    p.ml = ar.take<float>((size_t)n_chunks * 2 * t.n_heads * 2);
+    p.acc = ar.take<float>((size_t)n_chunks * 2 * t.n_heads * kv_width(t.head_dim));
   }
   return p;
 }
@@ -1155,7 +1161,7 @@ void launch_groups(const Attn& a, unsigned grid, hipStream_t stream) {
 int32_t attn(dci_ctx* ctx, const dci_attn& t, int type, Attn a, bool accumulate) {
   const Split s = split_of(t, type, accumulate);
   Arena ar(ctx->ws, ctx->ws_bytes);
-  const Parts parts = take_parts(ar, t, s, accumulate);
+  const Parts parts = take_parts(ar, t, s.n_chunks, accumulate);
   if (!ar.ok()) {
     ctx->req_workspace = ar.off;
     return fail(ctx, DCI_ERR_CAPACITY, "workspace holds %zu bytes, this attention call needs %zu", ctx->ws_bytes, ar.off);
@@ -1261,7 +1267,7 @@ size_t dci_attn_workspace_bytes(const dci_attn* attn, int32_t accumulate) {
   for (int type : {(int)dci::kE4M3, (int)attn->dtype}) {
     if (type != dci::kE4M3 && !dci::known_type(type)) return 0;
     dci::Arena ar(nullptr, 0);
-    (void)dci::take_parts(ar, *attn, dci::split_of(*attn, type, accumulate != 0), accumulate != 0);
+    (void)dci::take_parts(ar, *attn, dci::split_of(*attn, type, accumulate != 0).most_chunks, accumulate != 0);
     if (ar.off > most) most = ar.off;
   }
   return most;

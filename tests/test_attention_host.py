@@ -99,6 +99,33 @@ def test_no_launch_has_more_lanes_than_32_bits_count(lib, heads, kv, dim, edges)
     from paper_2503_01281_amd import binding as b
     a = b._Attn(n_rows=2 ** 31 - 1, n_edges=edges, n_src=10, max_list=0, n_heads=heads, kv_heads=kv, head_dim=dim)
     piece = 2 * 4 + -(-dim // 16) * 16 * 4
-    chunks = lib.dci_attn_workspace_bytes(C.byref(a), 0) // (2 * heads * piece)
+    chunks = (lib.dci_attn_workspace_bytes(C.byref(a), 0) - 2 * 255) // (2 * heads * piece)  # of two arrays on whole 256 bytes
     assert 0 < chunks * heads * 256 < 2 ** 32
     assert chunks * 2 ** 22 >= edges  # and a chunk stays one that a wavefront goes through in milliseconds
+
+
+@pytest.mark.parametrize("heads,kv,dim,dtype", [(4, 4, 64, 0), (16, 4, 64, 1), (32, 8, 128, 1), (128, 128, 16, 2), (1, 1, 1, 0), (8, 4, 128, 2), (128, 1, 256, 0)])
+@pytest.mark.parametrize("bias", [0, 1])
+def test_the_workspace_of_a_call_does_for_every_smaller_one(lib, heads, kv, dim, dtype, bias):
+    from paper_2503_01281_amd import binding as b
+
+    def need(edges, rows, max_list, accumulate):
+        a = b._Attn(n_rows=rows, n_edges=edges, n_src=10, max_list=max_list, n_heads=heads, kv_heads=kv, head_dim=dim, dtype=dtype,
+                    bias=64 if bias else None, bias_heads=bias)
+        return lib.dci_attn_workspace_bytes(C.byref(a), accumulate)
+
+    rng = np.random.default_rng(heads + dim)
+    # both sides of every place where chunks get longer, and sizes between
+    sizes = {0, 1, 64, 65, 2 ** 38} | {int(2 ** x) for x in rng.uniform(6, 38, 200)}
+    for chunk in (16, 32, 64, 128, 256, 512, 1024, 4096):
+        for waves in (1, 2, 3, 4, 8, 16, 32, 64, 128):
+            sizes |= {chunk * (wanted // waves + 1) + d for wanted in (1024, 4096) for d in (-1, 0, 1)}
+        sizes |= {min(2 ** 38, chunk * ((2 ** 24 - 1) // heads) + d) for d in (0, 1)}
+    for accumulate in (0, 1):
+        for max_list in (0, 64, 65, 1000):
+            needs = [need(e, 1000, max_list, accumulate) for e in sorted(sizes)]
+            assert needs == sorted(needs)
+        lists = [need(10 ** 6, 1000, m, accumulate) for m in (1, 64, 65, 10 ** 6, 2 * 10 ** 6, 0)]
+        assert lists == sorted(lists)
+        rows = [need(10 ** 6, r, 0, accumulate) for r in (0, 1, 999, 10 ** 6, 2 ** 31 - 1)]
+        assert rows == sorted(rows)

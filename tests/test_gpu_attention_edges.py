@@ -1,5 +1,5 @@
 """Attention over lists where its arithmetic and its launches end: infinite keys at every way that a head's columns lie on lanes, no
-sources, more pieces than one launch has workgroups for.
+sources, more pieces than one launch has workgroups for, workspaces sized for another call.
 
 Tolerances are those of attention_reference.attend."""
 import math
@@ -109,3 +109,29 @@ def test_more_chunks_and_heads_than_a_launch_has_workgroups():
         want = ref.attend(q[i:i + 1].double().cpu().numpy(), k.double().cpu().numpy(), v.double().cpu().numpy(), [0, e - b],
                           src[b:e].cpu().numpy().astype(np.int64), 0.25)
         check(out[i:i + 1], lse[i:i + 1], want, 1, "bf16")
+
+
+def test_a_workspace_sized_by_the_largest_call():
+    """A caller of the library who takes the workspace of the largest call has room for all smaller ones: here half as many, longer chunks need half."""
+    import ctypes as C
+
+    import paper_2503_01281_amd as dci
+    from paper_2503_01281_amd import binding as b
+    rng = np.random.default_rng(13)
+    heads, dim, sources = 4, 64, 100
+    k, v = (torch.from_numpy(rng.standard_normal((sources, heads, dim)).astype(np.float32)).cuda() for _ in range(2))
+    for largest, smaller in ((16_400, 16_384), (262_208, 262_144), (300_000, 40_000), (262_208, 65)):
+        ctx, args = dci.Context(0), {}
+        for edges in (largest, smaller):
+            indptr, src = lists([edges // 3, 0, edges - edges // 3], sources, rng)
+            q, out = torch.randn(3, heads, dim, device="cuda"), torch.empty(3, heads, dim, device="cuda")
+            args[edges] = (b._attn_args(q, heads, sources, dev(indptr), dev(src), out, 0.125, None, None, None, 0), q, out, indptr, src)
+        held = [dev(a[4]) for a in args.values()], [dev(a[3]) for a in args.values()]
+        for (a, *_), s, p in zip(args.values(), *held):
+            a.src, a.indptr = s.data_ptr(), p.data_ptr()
+        ctx.ensure_workspace(ctx.lib.dci_attn_workspace_bytes(C.byref(args[largest][0]), 0))
+        for edges, (a, q, out, indptr, src) in args.items():
+            ctx.check(ctx.lib.dci_attn_forward(ctx.handle, C.byref(a), k.data_ptr(), heads * dim, v.data_ptr(), heads * dim))
+            ctx.sync()
+            want = ref.attend(q.double().cpu().numpy(), k.double().cpu().numpy(), v.double().cpu().numpy(), indptr, src.astype(np.int64), 0.125)
+            check(out, None, want, 3, "fp32")
