@@ -497,9 +497,9 @@ typedef struct {
  * [0, n_slots)): nothing of its rows is read, whatever they hold.  A row that has nothing left gives out = 0 and lse = -inf.
  * Products, softmax statistics and sums are in fp32; out is rounded once to its type.  (Long lists of the cache whose query heads
  * share key heads, three or more to one, without bias, of 64, 128 or 256 columns: each weight times its value's scale is a sum of
- * three bf16 numbers, of two where more than five heads are worked on together, and at most 2^-18 of it is lost, more only where
- * that product is below 2^-100.)  Sums run in an order that follows from the arguments alone, so a call that is made again gives
- * the same bits. */
+ * three bf16 numbers, and at most 2^-27 of it is lost; of two where out has 16 bits and more than five heads are worked on together,
+ * then 2^-18; more only where that product is below 2^-100.)  Sums run in an order that follows from the arguments alone, so a call
+ * that is made again gives the same bits. */
 typedef struct {
   int64_t n_rows;          /* rows, or their bound where n_dev is given; 0 .. 2^31-1                     */
   const int64_t* n_dev;    /* device: the number of rows (nullable); rows from there on are left as they are */

@@ -657,9 +657,11 @@ __global__ __launch_bounds__(kAttnBlock, waves_per_simd(TYPE, GQ)) void k_attn_r
 //              (fp16) or three (fp32).  Column j is query head j % H, so every head comes 16 / H times.
 //   softmax    the lane that is left with a score holds four consecutive entries (4 b ..) of either tile, which is how the second product wants
 //              its operand: nothing is exchanged but the maximum over b.  Rescaling waits until a maximum grows.
-//   values     O = P V, 16 rows (column j of before) by 16 columns of V, 32 entries deep.  P is a sum of three bf16 numbers, two where H > 5
-//              (2^-27, 2^-18 of it are lost): part j / H of head j % H is row j, so the parts cost no instruction of their own.  The value's
-//              scale is P's.  A lane brings W / 16 bytes of eight entries' values, side by side over j, pairs two entries' bytes with v_perm
+//   values     O = P V, 16 rows (column j of before) by 16 columns of V, 32 entries deep.  P is a sum of three bf16 numbers (2^-27 of it is lost):
+//              part j / H of head j % H is row j, so the parts cost no instruction of their own.  Where H > 5 there are rows for two.  16-bit outputs
+//              have no use for the third (2^-18 of P is lost, a 128th of half a step of fp16), fp32 ones get it in a second product with the same
+//              operand (640,000 entries of eight key heads of 128 with 64 query heads 165 -> 167 us, four of 64 with 32 57 -> 61; in passes over
+//              four heads 256 and 85).  The value's scale is P's.  A lane brings W / 16 bytes of eight entries' values, side by side over j, pairs two entries' bytes with v_perm
 //              and converts.
 // At the end the parts of O are added up through LDS.  It does a quarter of the vector instructions of k_attn_chunks for four heads to a group:
 // 640,000 entries of eight key heads of 128 with 32 query heads take 281 to 297 us, 380 by k_attn_chunks.  What bounds it are the rows, 1.5 GB there
@@ -712,6 +714,7 @@ __global__ __launch_bounds__(kAttnBlock, W == 64 ? 3 : 2) void k_attn_groups(con
   const unsigned unit = blockIdx.x * kAttnWaves + wave, c = unit / (unsigned)a.passes, pass = unit - c * a.passes;
   const int kv = (int)pass / a.gq_passes, heads = a.pass_heads, h0 = (int)pass % a.gq_passes * heads;
   const int parts = heads <= 5 ? 3 : 2, part = j / heads;
+  const bool add_rest = NQ == 3 && parts == 2;
   const bool used = part < parts && h0 + j % heads < a.group;
   const int head = kv * a.group + min(h0 + j % heads, a.group - 1);
   const long long n = rows_of(a);
@@ -847,19 +850,22 @@ __global__ __launch_bounds__(kAttnBlock, W == 64 ? 3 : 2) void k_attn_groups(con
       DCI_EIGHT(DCI_SCALE)
 #undef DCI_SCALE
 #undef DCI_EIGHT
+      unsigned rest[4];  // what two parts leave, for fp32 outputs
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         float x = p[2 * i], y = p[2 * i + 1];
         unsigned w = bf16_pair(x, y);
-        if (part > 0) {
+        rest[i] = 0;
+        if (part > 0 || add_rest) {
           x -= __uint_as_float(w << 16);
           y -= __uint_as_float(w & 0xFFFF0000u);
-          w = bf16_pair(x, y);
-          if (part > 1) w = bf16_pair(x - __uint_as_float(w << 16), y - __uint_as_float(w & 0xFFFF0000u));
+          const unsigned w1 = bf16_pair(x, y), w2 = bf16_pair(x - __uint_as_float(w1 << 16), y - __uint_as_float(w1 & 0xFFFF0000u));
+          rest[i] = used && part == 0 ? w2 : 0;
+          if (part > 0) w = part > 1 ? w2 : w1;
         }
         pw[i] = used ? w : 0;
       }
-      const bf16x8 pa = __builtin_bit_cast(bf16x8, (u32x4{pw[0], pw[1], pw[2], pw[3]}));
+      const bf16x8 pa = __builtin_bit_cast(bf16x8, (u32x4{pw[0], pw[1], pw[2], pw[3]})), pr = __builtin_bit_cast(bf16x8, (u32x4{rest[0], rest[1], rest[2], rest[3]}));
 #pragma unroll
       for (int x = 0; x < kWords; ++x) {
         unsigned low[4], high[4];  // two entries' bytes 0 0' 1 1', 2 2' 3 3'
@@ -874,6 +880,7 @@ __global__ __launch_bounds__(kAttnBlock, W == 64 ? 3 : 2) void k_attn_groups(con
 #pragma unroll
           for (int i = 0; i < 4; ++i) u[i] = pair_of_codes(d < 2 ? low[i] : high[i], 1.f, d & 1);
           o[4 * x + d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pa, __builtin_bit_cast(bf16x8, u), o[4 * x + d], 0, 0, 0);
+          if (add_rest) o[4 * x + d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pr, __builtin_bit_cast(bf16x8, u), o[4 * x + d], 0, 0, 0);
         }
       }
     };

@@ -1,7 +1,7 @@
 """Attention over lists where its arithmetic and its launches end: infinite keys at every way that a head's columns lie on lanes, no
-sources, more pieces than one launch has workgroups for, workspaces sized for another call.
+sources, more pieces than one launch has workgroups for, workspaces sized for another call, weights of few bits.
 
-Tolerances are those of attention_reference.attend."""
+Tolerances are those of attention_reference.attend, or derived where they are used."""
 import math
 
 import numpy as np
@@ -135,3 +135,40 @@ def test_a_workspace_sized_by_the_largest_call():
             ctx.sync()
             want = ref.attend(q.double().cpu().numpy(), k.double().cpu().numpy(), v.double().cpu().numpy(), indptr, src.astype(np.int64), 0.125)
             check(out, None, want, 3, "fp32")
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("heads,kv", [(3, 1), (5, 1), (6, 1), (7, 1), (8, 1), (9, 1), (13, 1), (16, 2)])
+def test_weights_of_shared_key_heads_keep_the_bits_of_fp32(heads, kv, dim):
+    """Long lists of which two entries are left: values 0 with score 0 and values V with score -d, out = V / (1 + exp(d)), so that an error of the
+    second weight is the output's.  Scores are exact (one product each).  In units of 2^-24: 2.5 each for the weight's exponential, for that of a
+    rescaling and for that of a join (two in the last place, and the rounded argument times 0.1); 3 for the products with those in the accumulator,
+    and as many again, 10.5, in the sum; 5 for the additions of parts, pieces and the sum; 3 for the reciprocal and its product: 32 at most.  Two bf16
+    numbers can be off by 64 (2^-18)."""
+    import paper_2503_01281_amd as dci
+    ctx = dci.Context(0)
+    rng = np.random.default_rng(heads * 10 + dim)
+    n, each, n_slots = 250, 70, 4
+    codes = np.zeros((n_slots, 2, kv, dim), dtype=np.uint8)
+    codes[1, 0, :, 0] = 0x38  # a key of (1, 0, 0, ...)
+    codes[1, 1] = rng.integers(0x30, 0x60, (kv, dim))
+    scales = np.ones((n_slots, kv, 2), dtype=np.float32)
+    cache = dci.KvCache.from_arrays(dev(codes), dev(scales), None, None, dim, 1)
+    values = ref.e4m3_values()[codes]
+    src = np.full((n, each), -1, dtype=np.int32)
+    for i in range(n):
+        src[i, np.sort(rng.permutation(each)[:2])] = rng.permutation(2)
+    indptr = np.arange(0, n * each + 1, each)
+    q = np.zeros((n, heads, dim), dtype=np.float32)
+    q[:, :, 0] = -rng.uniform(0.002, 0.1, (n, heads))
+    want = ref.attend(q.astype(np.float64), values[:, 0], values[:, 1], indptr, src.ravel().astype(np.int64), 1.0)
+    for dtype in ("fp32", "bf16"):
+        if dtype == "bf16":
+            q = rounded(q, dtype).float().numpy()
+            want = ref.attend(q.astype(np.float64), values[:, 0], values[:, 1], indptr, src.ravel().astype(np.int64), 1.0)
+        out, lse = torch.empty(n, heads, dim, dtype=TYPES[dtype], device="cuda"), torch.empty(n, heads, device="cuda")
+        dci.dci_attn_cached(ctx, rounded(q, dtype).cuda(), cache, dev(indptr), dev(src.ravel()), out, 1.0, lse=lse)
+        ctx.sync()
+        # with 16 bits a weight of two parts may be off by 2^-18 more
+        off = 32 * ref.U if dtype == "fp32" else 32 * ref.U + 2.0 ** -18
+        check(out, lse, want[:3] + (off * np.abs(want[0]),) + want[4:], n, dtype)
