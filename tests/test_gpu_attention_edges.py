@@ -172,3 +172,48 @@ def test_weights_of_shared_key_heads_keep_the_bits_of_fp32(heads, kv, dim):
         # with 16 bits a weight of two parts may be off by 2^-18 more
         off = 32 * ref.U if dtype == "fp32" else 32 * ref.U + 2.0 ** -18
         check(out, lse, want[:3] + (off * np.abs(want[0]),) + want[4:], n, dtype)
+
+
+@pytest.mark.parametrize("heads,kv,dim,dtype", [(4, 1, 64, "fp32"), (8, 1, 128, "bf16"), (3, 1, 256, "fp16"), (16, 2, 64, "fp32")])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_left_out_entries_of_shared_key_heads_may_hold_anything(heads, kv, dim, dtype, accumulate):
+    """Slots that only left-out entries stand beside, slot 0 among them, hold codes of no number; the result is that of a cache with zeros there."""
+    import paper_2503_01281_amd as dci
+    from tests.test_gpu_attention import make_cache
+    ctx = dci.Context(0)
+    rng = np.random.default_rng(dim + heads)
+    n_slots, sources, lengths = 90, 60, [70, 300, 0, 129, 66, 1000]
+    cache, _ = make_cache(dci, n_slots, kv, dim, 16, rng)
+    slots = (rng.permutation(n_slots - 20)[:sources] + 20).astype(np.int32)  # slots 0 .. 19 are named by nobody
+    slots[rng.random(sources) < 0.3] = -1
+    indptr, src = lists(lengths, sources, rng, outside=0.1)
+    q = torch.randn(len(lengths), heads, dim, device="cuda").to(TYPES[dtype])
+    before, got = cache.weight.clone(), []
+    for code in (0, 0x7F, 0xFF):
+        cache.codes[:20] = code
+        cache.codes[20:][~torch.isin(torch.arange(20, n_slots, device="cuda"), dev(slots))] = code
+        cache.weight.copy_(before)
+        out, lse = torch.empty_like(q), torch.empty(len(lengths), heads, device="cuda")
+        dci.dci_attn_cached(ctx, q, cache, dev(indptr), dev(src), out, 0.1, slots=dev(slots), lse=lse, accumulate=accumulate)
+        ctx.sync()
+        got.append((out, lse, cache.weight.clone()))
+    assert torch.isfinite(got[0][0].float()).all()
+    for other in got[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(got[0], other))
+
+
+def test_a_call_that_needs_no_workspace_is_taken_without_one():
+    import ctypes as C
+
+    import paper_2503_01281_amd as dci
+    from paper_2503_01281_amd import binding as b
+    ctx = dci.Context(0)
+    cache = dci.KvCache(ctx, 32, 2, 32)
+    q, out = torch.zeros(4, 2, 32, device="cuda"), torch.zeros(4, 2, 32, device="cuda")
+    indptr, src = torch.zeros(5, dtype=torch.int64, device="cuda"), torch.zeros(64, dtype=torch.int32, device="cuda")
+    for edges in (8, 64):
+        a = b._attn_args(q, 2, 0, indptr, src[:edges], out, 1.0, None, None, None, 0)
+        for accumulate in (0, 1):
+            assert ctx.lib.dci_attn_workspace_bytes(C.byref(a), accumulate) == 0
+            assert ctx.lib.dci_attn_cached(ctx.handle, C.byref(a), C.byref(cache.c), None, accumulate) == 0
+    ctx.sync()
