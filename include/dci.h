@@ -540,7 +540,8 @@ int32_t dci_attn_forward(dci_ctx* ctx, const dci_attn* attn, const void* k, int6
  * and kv_heads must be the cache's. */
 int32_t dci_attn_cached(dci_ctx* ctx, const dci_attn* attn, const dci_kv_cache* cache, const int32_t* slots, int32_t accumulate);
 
-/* Empties the cache: scales, weights and codes 0, nodes -1 (weight and node may be NULL). */
+/* Empties the cache: scales, weights and codes 0, nodes -1 (weight and node may be NULL).  A remap that dci_kv_admit keeps beside it is the
+ * caller's to set to -1. */
 int32_t dci_kv_clear(dci_ctx* ctx, const dci_kv_cache* cache);
 
 /* Writes rows of keys and values into the cache.  slots: device int32 [n_max], STRICTLY ASCENDING; entries outside [0, n_slots) are

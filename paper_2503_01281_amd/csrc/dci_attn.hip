@@ -19,10 +19,11 @@
 // indptr).  A list that lies within a chunk is done there; of others (m, l, acc) of the piece is left in the workspace, for k_attn_join to add up in
 // order.  A chunk has at most two such pieces: that of a list that goes on from before or begins with the chunk (0), and that of one that begins
 // inside and goes on behind it (1).
-// What bounds it: the rows that entries name, line by line.  98,304 rows of 12 entries of four 8-bit heads of 64, with weights: 140 us (129 without
-// them), 0.92 GB between L2 and memory by the counters, 6.5 TB/s.  Dense 32-bit rows, 24,576 by 9 entries of 2 KB: 71 us, 0.47 GB, 6.6 TB/s.
-// Where rows are few or entries narrow it is the chain of reads, bounds - source - slot - row: 10,007 rows of 20 entries of three heads of 41 with
-// biases and weights take 47 us at 2.7 TB/s.
+// What bounds it: the lines that entries name.  98,304 rows of 12 entries of four 8-bit heads of 64, with weights: 141 us (129 without them), 0.92 GB
+// between L2 and memory by the counters, 6.5 TB/s; 0.6 GB of them are keys and values, 0.1 q and out, the rest lines of slots, scales and weights.
+// Dense 32-bit rows, 24,576 by 8.5 entries of 2 KB: 72 us, 0.47 GB, 6.5 TB/s.  Where rows are few or entries narrow it is the chain of reads, bounds -
+// source - slot - row, and the instructions: 10,007 rows of 36 entries of three heads of 41 with biases and weights take 47 us at 2.7 TB/s, of which
+// 14.8 million vector instructions are 24.
 #include "dci_kv.h"
 
 namespace dci {
@@ -31,7 +32,10 @@ namespace {
 constexpr int kAttnBlock = 256, kAttnWaves = kAttnBlock / kWave;
 constexpr int kShort = 64;  // longer lists are worked on by chunks
 constexpr float kLog2E = 1.44269504088896340736f;
-// wavefronts to a SIMD that the registers are shared out for: as many as there are without spilling
+// Wavefronts to a SIMD that the registers are shared out for: as many as there are with few registers spilled.  (Two query heads to a key head spill up
+// to 36 with three wavefronts, of 8-bit and 32-bit rows.  With two wavefronts and none spilled, lists of nine to 2,000 entries of four such pairs
+// take 2 % more on average: 10 to 1 % less with a bias where lists are short, 1 to 14 % more where rows are of 8 bits and lists long, 9 to 23 % more
+// for 16-bit rows and short lists, which spill none.)
 constexpr int waves_per_simd(int type, int gq) { return gq == 4 ? 2 : gq == 2 ? 3 : type == DCI_F32 || type == kE4M3 ? 3 : 4; }
 // columns to a lane
 template <int TYPE>
@@ -660,12 +664,12 @@ __global__ __launch_bounds__(kAttnBlock, waves_per_simd(TYPE, GQ)) void k_attn_r
 //   values     O = P V, 16 rows (column j of before) by 16 columns of V, 32 entries deep.  P is a sum of three bf16 numbers (2^-27 of it is lost):
 //              part j / H of head j % H is row j, so the parts cost no instruction of their own.  Where H > 5 there are rows for two.  16-bit outputs
 //              have no use for the third (2^-18 of P is lost, a 128th of half a step of fp16), fp32 ones get it in a second product with the same
-//              operand (640,000 entries of eight key heads of 128 with 64 query heads 165 -> 167 us, four of 64 with 32 57 -> 61; in passes over
-//              four heads 256 and 85).  The value's scale is P's.  A lane brings W / 16 bytes of eight entries' values, side by side over j, pairs two entries' bytes with v_perm
+//              operand (620,000 entries of eight key heads of 128 with 64 query heads 295 -> 299 us, of four of 64 with 32 96 -> 100; in passes
+//              over four heads half as many take 256 for 165, and 85 for 57).  The value's scale is P's.  A lane brings W / 16 bytes of eight entries' values, side by side over j, pairs two entries' bytes with v_perm
 //              and converts.
 // At the end the parts of O are added up through LDS.  It does a quarter of the vector instructions of k_attn_chunks for four heads to a group:
-// 640,000 entries of eight key heads of 128 with 32 query heads take 281 to 297 us, 380 by k_attn_chunks.  What bounds it are the rows, 1.5 GB there
-// by the counters, 5 to 5.4 TB/s; a million entries of four heads of 64 take 117 us at 4.8 TB/s, with 80 requests to L2 a nanosecond.
+// 620,000 entries of eight key heads of 128 with 32 query heads take 280 to 299 us, 380 by k_attn_chunks.  What bounds it are the rows, 1.5 GB there
+// by the counters, 5 to 5.4 TB/s; 950,000 entries of four heads of 64 take 116 us at 4.9 TB/s, with 82 requests to L2 a nanosecond.
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -859,8 +863,10 @@ __global__ __launch_bounds__(kAttnBlock, W == 64 ? 3 : 2) void k_attn_groups(con
         if (part > 0 || add_rest) {
           x -= __uint_as_float(w << 16);
           y -= __uint_as_float(w & 0xFFFF0000u);
-          const unsigned w1 = bf16_pair(x, y), w2 = bf16_pair(x - __uint_as_float(w1 << 16), y - __uint_as_float(w1 & 0xFFFF0000u));
-          rest[i] = used && part == 0 ? w2 : 0;
+          const unsigned w1 = bf16_pair(x, y);
+          unsigned w2 = 0;
+          if (NQ == 3 || part > 1) w2 = bf16_pair(x - __uint_as_float(w1 << 16), y - __uint_as_float(w1 & 0xFFFF0000u));
+          if (add_rest) rest[i] = used && part == 0 ? w2 : 0;
           if (part > 0) w = part > 1 ? w2 : w1;
         }
         pw[i] = used ? w : 0;
@@ -1051,7 +1057,7 @@ struct Split {
   int64_t n_chunks;
   int64_t most_chunks;  // that this call or one of fewer entries has, which may be cut shorter
 };
-constexpr int64_t kMaxGroups = 0xFFFFFFFFll / kAttnBlock;  // workgroups to a launch, whose lanes are counted in 32 bits
+constexpr int64_t kMaxGroups = 0xFFFFFFFFll / kAttnBlock;  // workgroups to a launch: its lanes are counted in 32 bits, and one of more runs too few
 constexpr int64_t kWantedWaves = 4096, kFewWaves = 1024;  // 16 and four to a compute unit
 constexpr int kStashHeads = 32;  // query heads of a wavefront, at most, with weights: 40 KB of scores to a workgroup, four workgroups to a compute unit
 
@@ -1071,11 +1077,11 @@ Split split_of(const dci_attn& t, int type, bool accumulate) {
   s.p_log2 = log2_up((int64_t)s.wave_heads << s.lh_log2);
   if (s.p_log2 < 2) s.p_log2 = 2;  // entries are taken four at a time
   s.passes = (t.kv_heads + s.wave_heads - 1) / s.wave_heads * s.gq_passes;
-  // To k_attn_groups from three query heads to a key head on: 640,000 entries of eight key heads of 128 take 297 us there for three to a group and 385 in
-  // k_attn_chunks, 306 and 700 for eight; for two 294 and 261 (a million entries of four of 64: 132 and 169, 146 and 289; 127 and 114).
+  // To k_attn_groups from three query heads to a key head on: 620,000 entries of eight key heads of 128 take 297 us there for three to a group and 385 in
+  // k_attn_chunks, 306 and 700 for eight; for two 294 and 261 (950,000 entries of four of 64: 132 and 169, 146 and 289; 127 and 114).
   s.matrix = type == kE4M3 && group >= 3 && !t.bias && (t.head_dim == 64 || t.head_dim == 128 || t.head_dim == 256);
   const int64_t waves = s.matrix ? (int64_t)t.kv_heads * ((group + 7) / 8) : ((int64_t)t.kv_heads * kv_width(t.head_dim) + 1023) / 1024 * ((group + gq - 1) / gq);
-  // Chunks of 64 to 512 entries: as long as there are wavefronts enough (with half as many 640,000 entries of eight heads of 128, two query heads to
+  // Chunks of 64 to 512 entries: as long as there are wavefronts enough (with half as many 620,000 entries of eight heads of 128, two query heads to
   // each, take 309 us for 261).  Shorter ones (16 or 32; a step of k_attn_groups is 32 entries) where that leaves only a few to a compute unit: 28,000
   // entries of seven 32-bit heads of 64 take 48 us in chunks of 32 and 55 in chunks of 64.  With more wavefronts the pieces cost more than they give:
   // 37,000 entries of eight 16-bit heads of 128 on two take 46 us in chunks of 16, 38 in 32, 37 in 64.
@@ -1209,8 +1215,10 @@ int32_t attn(dci_ctx* ctx, const dci_attn& t, int type, Attn a, bool accumulate)
   a.n_chunks = (int)s.n_chunks;
   a.longest = t.max_list > 0 ? t.max_list : t.n_edges;
   const bool by_row = t.n_rows <= s.n_chunks;
-  // A handful of rows: all by chunks, which spares a launch (305 -> 298 us for 16 long lists), and a row that has nothing is the join's.  With many,
-  // a chunk might hold dozens of tiny lists, and a wavefront takes several microseconds for each.
+  // A handful of rows: all by chunks, which spares a launch, and a row that has nothing is the join's: 16 lists of 500 entries take 16 to 17 us and 17
+  // of them 22 to 30, of 10,000 entries 35 to 63 and 41 to 71 (four key heads of 64; dense 32-bit rows, 8-bit ones, 8-bit ones of four query heads each).
+  // With many rows a chunk might hold dozens of tiny lists, and a wavefront takes several microseconds for each; how many may go before that costs
+  // more than the launch depends on their lengths, which are not known here, so 16 is a line on the safe side and not the best one.
   const bool all_by_chunks = by_row && t.n_rows <= 16;
   a.short_list = all_by_chunks ? 0 : kShort;
   // lane groups to a row: one, unless that leaves wavefronts to be had (no more then than there are entries in a list) or, with weights, the scores

@@ -182,7 +182,7 @@ __device__ void write_block(const KvWrite& a, int kind, int head, long long i, i
 // slots come first, as entries outside the cache have no rows (0 to 3 % slower than all rows at once for half a million rows, 1 to 8 % quicker
 // for fewer), then all rows, keys and values.  The blocks that end among the wavefront's entries are done side by side, their maxima joined in LDS; one that goes on behind them, and one whose other rows have to be rounded
 // anew, is done on its own (write_block).  What bounds it: the rows' bytes, read and written once (half a million rows of 512 numbers in 16 bits:
-// 149 to 176 us, by what the last-level cache has of them, 0.78 GB, 4.4 to 5.2 TB/s).
+// 142 to 176 us, by what the last-level cache has of them, 0.78 GB, 4.4 to 5.5 TB/s).
 template <int TYPE, int T>
 __global__ __launch_bounds__(kKvBlock) void k_kv_write(const KvWrite a) {
   const int lane = lane_id(), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave);
